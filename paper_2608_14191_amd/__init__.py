@@ -15,3 +15,12 @@ from ._lib import (  # noqa: F401
     aatc_group_decode_workspace_bytes, aatc_group_encode, aatc_group_params_bytes,
     aatc_group_params_pack,
 )
+from ._paged import (  # noqa: F401
+    ROPE_BANDS, ROPE_HALF, ROPE_INTERLEAVED, ROPE_LINEAR, ROPE_NTK, ROPE_PLAIN, ROPE_YARN,
+    PagedCache, PageTable, Rope,
+    aatc_decode_attention_paged, aatc_decode_paged_workspace_bytes, aatc_paged_append,
+    aatc_paged_decode_attention, aatc_paged_decode_workspace_bytes, aatc_pages_compact,
+    aatc_pages_copy, aatc_pages_fork, aatc_pages_free, aatc_pages_reserve,
+    aatc_pages_workspace_bytes, aatc_rope, aatc_rope_frequencies,
+)
+from ._lib import F16  # noqa: F401

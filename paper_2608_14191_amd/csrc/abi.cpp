@@ -171,15 +171,13 @@ extern "C" size_t aatc_decode_workspace_bytes(int32_t batch, int32_t n_q_heads,
   return decode_workspace_bytes(batch, n_q_heads, n_kv_heads, cap);
 }
 
-namespace {
-
-aatc_status check_decode(const void* dev_params_k, const void* dev_params_v, int32_t batch,
-                         int32_t n_q_heads, int32_t n_kv_heads, int32_t d, const void* q,
-                         aatc_dtype q_dtype, const void* k_codes, const uint16_t* k_alpha,
-                         const void* v_codes, const uint16_t* v_alpha, const int32_t* seq_len,
-                         int64_t cap, int32_t k_record_bytes, int32_t v_record_bytes,
-                         float softmax_scale, const float* out, const void* workspace,
-                         size_t ws_bytes, bool static_ws = false) {
+aatc_status aatc::check_decode(const void* dev_params_k, const void* dev_params_v, int32_t batch,
+                               int32_t n_q_heads, int32_t n_kv_heads, int32_t d, const void* q,
+                               aatc_dtype q_dtype, const void* k_codes, const uint16_t* k_alpha,
+                               const void* v_codes, const uint16_t* v_alpha, const int32_t* seq_len,
+                               int64_t cap, int32_t k_record_bytes, int32_t v_record_bytes,
+                               float softmax_scale, const float* out, const void* workspace,
+                               size_t ws_bytes, bool static_ws) {
   if (d != kD) return AATC_E_UNSUPPORTED;
   if (!dev_params_k || !dev_params_v || !q || !k_codes || !k_alpha || !v_codes || !v_alpha ||
       !seq_len || !out || (!workspace && !static_ws))
@@ -207,6 +205,8 @@ aatc_status check_decode(const void* dev_params_k, const void* dev_params_v, int
   }
   return AATC_OK;
 }
+
+namespace {
 
 aatc_status check_new_tokens(const void* x_k, const void* x_v, aatc_dtype x_dtype) {
   if (!x_k || !x_v) return AATC_E_INVALID;

@@ -25,6 +25,7 @@
 #include "decode_plan.h"
 #include "encode_core.h"
 #include "launch.h"
+#include "paged.h"
 #include "params.h"
 #include "workspace.h"
 
@@ -2510,14 +2511,23 @@ static aatc_status launch_mfma_nt(const DecodeArgs& a, const MfmaPlan& p, hipStr
                       : launch_mfma_np<NT, 4, APPEND>(a, p.np, st);
 }
 
-aatc_status launch_decode(const void* params_k, const void* params_v, int batch,
-                          int n_q_heads, int n_kv_heads, const void* q, aatc_dtype q_dtype,
-                          const void* k_codes, const uint16_t* k_alpha, const void* v_codes,
-                          const uint16_t* v_alpha, const int32_t* seq_len, int64_t cap,
-                          int rk, int rv, float softmax_scale, float* out, void* workspace,
-                          void* stream, const void* x_k, const void* x_v, aatc_dtype x_dtype,
-                          int counter_rows, const void* seg_k, const void* seg_v,
-                          aatc_dtype seg_dtype, const int32_t* seg_len, int seg_cap) {
+namespace {
+
+// A paged segment (launch_decode_paged): its attention's arguments, type and workspace.
+struct PagedSegment {
+  const PagedArgs& args;
+  aatc_dtype dtype;
+  void* workspace;
+};
+
+aatc_status decode(const void* params_k, const void* params_v, int batch, int n_q_heads,
+                   int n_kv_heads, const void* q, aatc_dtype q_dtype, const void* k_codes,
+                   const uint16_t* k_alpha, const void* v_codes, const uint16_t* v_alpha,
+                   const int32_t* seq_len, int64_t cap, int rk, int rv, float softmax_scale,
+                   float* out, void* workspace, void* stream, const void* x_k, const void* x_v,
+                   aatc_dtype x_dtype, int counter_rows, const void* seg_k, const void* seg_v,
+                   aatc_dtype seg_dtype, const int32_t* seg_len, int seg_cap,
+                   const PagedSegment* paged) {
   const int G = n_q_heads / n_kv_heads;
   const WsLayout wl = ws_layout(batch, n_q_heads, n_kv_heads, cap, counter_rows);
   char* ws = static_cast<char*>(workspace);
@@ -2547,6 +2557,13 @@ aatc_status launch_decode(const void* params_k, const void* params_v, int batch,
                        softmax_scale * kLog2e, sp);
     if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
     seg = sp;
+  }
+  if (paged) {
+    PagedArgs pa = paged->args;
+    pa.seg = reinterpret_cast<Partial*>(ws + wl.seg);
+    const aatc_status e = launch_paged(pa, paged->dtype, paged->workspace, stream);
+    if (e != AATC_OK) return e;
+    seg = pa.seg;
   }
   // A new token's append is part of the matrix-core launch where that has one workgroup row per
   // KV head; other shapes run the per-token encode first.
@@ -2602,6 +2619,35 @@ aatc_status launch_decode(const void* params_k, const void* params_v, int batch,
                      static_cast<const uint8_t*>(v_codes), v_alpha, seq_len, cap,
                      softmax_scale, out, ctr, parts, n_splits, rk, rv, seg);
   return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
+}
+
+}  // namespace
+
+aatc_status launch_decode(const void* params_k, const void* params_v, int batch,
+                          int n_q_heads, int n_kv_heads, const void* q, aatc_dtype q_dtype,
+                          const void* k_codes, const uint16_t* k_alpha, const void* v_codes,
+                          const uint16_t* v_alpha, const int32_t* seq_len, int64_t cap,
+                          int rk, int rv, float softmax_scale, float* out, void* workspace,
+                          void* stream, const void* x_k, const void* x_v, aatc_dtype x_dtype,
+                          int counter_rows, const void* seg_k, const void* seg_v,
+                          aatc_dtype seg_dtype, const int32_t* seg_len, int seg_cap) {
+  return decode(params_k, params_v, batch, n_q_heads, n_kv_heads, q, q_dtype, k_codes, k_alpha,
+                v_codes, v_alpha, seq_len, cap, rk, rv, softmax_scale, out, workspace, stream,
+                x_k, x_v, x_dtype, counter_rows, seg_k, seg_v, seg_dtype, seg_len, seg_cap,
+                nullptr);
+}
+
+aatc_status launch_decode_paged(const void* params_k, const void* params_v, int batch,
+                                int n_q_heads, int n_kv_heads, const void* q, aatc_dtype q_dtype,
+                                const void* k_codes, const uint16_t* k_alpha, const void* v_codes,
+                                const uint16_t* v_alpha, const int32_t* seq_len, int64_t cap,
+                                int rk, int rv, float softmax_scale, float* out, void* workspace,
+                                void* stream, const PagedArgs& pages, aatc_dtype pages_dtype,
+                                void* pages_workspace) {
+  const PagedSegment segment{pages, pages_dtype, pages_workspace};
+  return decode(params_k, params_v, batch, n_q_heads, n_kv_heads, q, q_dtype, k_codes, k_alpha,
+                v_codes, v_alpha, seq_len, cap, rk, rv, softmax_scale, out, workspace, stream,
+                nullptr, nullptr, AATC_BF16, 0, nullptr, nullptr, AATC_BF16, nullptr, 0, &segment);
 }
 
 }  // namespace aatc

@@ -24,6 +24,15 @@ aatc_status launch_encode_last(const void* params, int n_heads, int batch, const
                                uint16_t* alpha, int64_t cap, int record_bytes,
                                const int32_t* seq_len, void* stream);
 
+// What every decode entry point asks of its arguments (abi.cpp).
+aatc_status check_decode(const void* dev_params_k, const void* dev_params_v, int32_t batch,
+                         int32_t n_q_heads, int32_t n_kv_heads, int32_t d, const void* q,
+                         aatc_dtype q_dtype, const void* k_codes, const uint16_t* k_alpha,
+                         const void* v_codes, const uint16_t* v_alpha, const int32_t* seq_len,
+                         int64_t cap, int32_t k_record_bytes, int32_t v_record_bytes,
+                         float softmax_scale, const float* out, const void* workspace,
+                         size_t ws_bytes, bool static_ws = false);
+
 // counter_rows: see ws_layout (0: the call's own rows).
 size_t decode_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int64_t cap,
                               int counter_rows = 0);

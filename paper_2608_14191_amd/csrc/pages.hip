@@ -1,0 +1,376 @@
+// Page tables on the device: fork, free, reserve, compact and copy.
+//
+// Whole numbers and moved bytes only.  Counts change by atomic additions, whose order does not
+// matter; which free page goes where follows from prefix sums in the order of the pages and the
+// rows, taken by one workgroup (a table's bookkeeping is a few thousand numbers, and its time
+// that of a few dependent memory accesses).  Copies are bound by memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "paged.h"
+
+namespace aatc {
+namespace {
+
+constexpr int kListThreads = 256;
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr int kPlanPages = 16;                  // pages per thread and step of a scan
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// Exclusive prefix sum of v over a workgroup of kPlanThreads; total in `sum`.  (Two barriers:
+// the scratch is free again at the return.)
+__device__ inline int block_scan(int v, int& sum, int* scratch) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(incl, o, 64);
+    incl += lane >= o ? up : 0;
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    before += w < wave ? scratch[w] : 0;
+    all += scratch[w];
+  }
+  __syncthreads();
+  sum = all;
+  return before + incl - v;
+}
+
+// ---------------------------------------------------------------------------------------
+// Fork: a workgroup per pair.
+__global__ __launch_bounds__(kListThreads) void fork_kernel(
+    const int32_t* __restrict__ src, int64_t src_stride, int src_rows, int32_t* __restrict__ dst,
+    int64_t dst_stride, int dst_rows, int entries, int32_t* __restrict__ ref, int n_pages,
+    const int32_t* __restrict__ pairs, int64_t n) {
+  const int64_t i = blockIdx.x;
+  const int from = pairs[2 * i], to = pairs[2 * i + 1];
+  if (from < 0 || from >= src_rows || to < 0 || to >= dst_rows) return;      // (uniform)
+  // A later pair with the same destination (and a source that exists) takes it.
+  int later = 0;
+  for (int64_t j = i + 1 + threadIdx.x; j < n; j += kListThreads)
+    later |= pairs[2 * j + 1] == to && pairs[2 * j] >= 0 && pairs[2 * j] < src_rows;
+  if (__syncthreads_or(later)) return;
+  for (int e = threadIdx.x; e < entries; e += kListThreads) {
+    const int page = src[from * src_stride + e];
+    dst[to * dst_stride + e] = page;
+    if (page >= 0 && page < n_pages) atomicAdd(&ref[page], 1);
+  }
+}
+
+// Free: a workgroup per listed row; the exchange gives each entry to one of the workgroups that
+// a row listed twice has.
+__global__ __launch_bounds__(kListThreads) void free_kernel(int32_t* table, int64_t stride,
+                                                            int rows, int entries, int32_t* ref,
+                                                            int n_pages,
+                                                            const int32_t* __restrict__ list) {
+  const int row = list[blockIdx.x];
+  if (row < 0 || row >= rows) return;
+  for (int e = threadIdx.x; e < entries; e += kListThreads) {
+    const int page = atomicExch(&table[row * stride + e], -1);
+    if (page >= 0 && page < n_pages) atomicAdd(&ref[page], -1);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Reserve: one workgroup.  Workspace: for every row the first of its places in the list of free
+// pages to hand out, its partial page to leave (-1: none), then that list.
+struct ReserveSpace {
+  int32_t *place, *leave, *free;
+};
+__host__ __device__ inline ReserveSpace reserve_space(void* ws, int64_t rows) {
+  auto* p = static_cast<int32_t*>(ws);
+  return {p, p + rows, p + 2 * rows};
+}
+
+__global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
+    int32_t* table, int64_t stride, int rows, int entries, int32_t* ref, int n_pages, int shift,
+    int len_max, const int32_t* __restrict__ held, const int32_t* __restrict__ wanted,
+    int32_t* pairs, int32_t* lacking, void* ws) {
+  __shared__ int scratch[kPlanWaves];
+  __shared__ int chunk[kPlanThreads];
+  const int tid = threadIdx.x;
+  const ReserveSpace sp = reserve_space(ws, rows);
+  const int mask = (1 << shift) - 1;
+  // Row r: tokens from .. to - 1 to come.
+  struct Row {
+    int from, to;
+    __device__ bool grows() const { return to > from; }
+  };
+  auto row_of = [&](int r) {
+    return Row{min(max(held[r], 0), len_max), min(max(wanted[r], 0), len_max)};
+  };
+  // The begun page that row r's first new token falls into (-1: none).
+  auto partial_of = [&](int r, const Row& w) {
+    if (!w.grows() || !(w.from & mask)) return -1;
+    const int page = table[r * stride + (w.from >> shift)];
+    return page >= 0 && page < n_pages ? page : -1;
+  };
+  auto new_pages = [&](const Row& w) {
+    return w.grows() ? ((w.to + mask) >> shift) - ((w.from + mask) >> shift) : 0;
+  };
+  // (1) What each row needs: a page in the place of one that others hold too, unless every other
+  // holder is an earlier row of this call that gets a copy, and its new pages.
+  int demand = 0;
+  for (int base = 0; base < rows; base += kPlanThreads) {
+    const int r = base + tid;
+    const Row w = r < rows ? row_of(r) : Row{0, 0};
+    const int mine = r < rows ? partial_of(r, w) : -1;
+    const int count = mine >= 0 ? ref[mine] : 0;
+    int earlier = 0;
+    if (__syncthreads_or(count > 1)) {
+      for (int b = 0; b <= base; b += kPlanThreads) {
+        const int other = b + tid;
+        int page = -1;
+        if (b == base) page = mine;
+        else page = partial_of(other, row_of(other));
+        __syncthreads();
+        chunk[tid] = page;
+        __syncthreads();
+        if (count > 1) {
+          const int upto = b == base ? tid : kPlanThreads;
+          for (int k = 0; k < upto; ++k) earlier += chunk[k] == mine;
+        }
+      }
+    }
+    const bool copy = count - earlier > 1;
+    int sum = 0;
+    const int place = block_scan((copy ? 1 : 0) + new_pages(w), sum, scratch);
+    if (r < rows) {
+      sp.place[r] = demand + place;
+      sp.leave[r] = copy ? mine : -1;
+    }
+    demand += sum;
+  }
+  // (2) The lowest free pages, as many.
+  int found = 0;
+  for (int64_t base = 0; base < n_pages && found < demand; base += kPlanThreads * kPlanPages) {
+    const int64_t p0 = base + tid * kPlanPages;
+    unsigned open = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanPages; ++k)
+      if (p0 + k < n_pages && ref[p0 + k] <= 0) open |= 1u << k;
+    int sum = 0;
+    int place = found + block_scan(__popc(open), sum, scratch);
+    while (open && place < demand) {
+      sp.free[place++] = (int)p0 + __builtin_ctz(open);
+      open &= open - 1;
+    }
+    found += sum;
+  }
+  __syncthreads();                              // (the list is this workgroup's own)
+  const bool enough = found >= demand;
+  if (tid == 0) *lacking = enough ? 0 : demand - found;
+  // (3) Hand out.
+  for (int r = tid; r < rows; r += kPlanThreads) {
+    const int old = enough ? sp.leave[r] : -1;
+    int now = -1;
+    if (old >= 0) {
+      now = sp.free[sp.place[r]];
+      table[r * stride + (row_of(r).from >> shift)] = now;
+      atomicAdd(&ref[old], -1);
+      ref[now] = 1;
+    }
+    pairs[2 * r] = old;
+    pairs[2 * r + 1] = now;
+  }
+  if (!enough) return;
+  for (int i = tid; i < demand; i += kPlanThreads) {
+    int lo = 0, hi = rows - 1;                  // the last row whose places begin at or before i
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (sp.place[mid] <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    const int k = i - sp.place[lo] - (sp.leave[lo] >= 0 ? 1 : 0);
+    if (k < 0) continue;                        // the copy's
+    const int page = sp.free[i];
+    table[lo * stride + ((row_of(lo).from + mask) >> shift) + k] = page;
+    ref[page] = 1;
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Compact: where each page goes (one workgroup), then the table (all of them).  Workspace: the
+// new place of every page.
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const int32_t* ref,
+                                                                    int n_pages, int32_t* ref_out,
+                                                                    int32_t* pairs,
+                                                                    int32_t* moves, int32_t* to) {
+  __shared__ int scratch[kPlanWaves];
+  const int tid = threadIdx.x;
+  constexpr int kStep = kPlanThreads * kPlanPages;
+  int live = 0;
+  for (int64_t base = 0; base < n_pages; base += kStep) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanPages; ++k) {
+      const int64_t p = base + k * kPlanThreads + tid;
+      n += p < n_pages && ref[p] > 0;
+    }
+    int sum = 0;
+    block_scan(n, sum, scratch);
+    live += sum;
+  }
+  // Pages in use from `live` on, and free ones below it: as many of one as of the other.
+  int movers = 0, holes = 0;
+  for (int64_t base = 0; base < n_pages; base += kStep) {
+    const int64_t p0 = base + (int64_t)tid * kPlanPages;
+    unsigned go = 0, open = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanPages; ++k) {
+      const int64_t p = p0 + k;
+      if (p >= n_pages) continue;
+      const bool used = ref[p] > 0;
+      go |= (used && p >= live) ? 1u << k : 0u;
+      open |= (!used && p < live) ? 1u << k : 0u;
+      to[p] = (int)p;
+    }
+    int sum = 0;
+    int at = movers + block_scan(__popc(go), sum, scratch);
+    movers += sum;
+    for (; go; go &= go - 1) pairs[2 * at++] = (int)p0 + __builtin_ctz(go);
+    at = holes + block_scan(__popc(open), sum, scratch);
+    holes += sum;
+    for (; open; open &= open - 1) pairs[2 * at++ + 1] = (int)p0 + __builtin_ctz(open);
+  }
+  __syncthreads();
+  if (tid == 0) *moves = movers;
+  // (ref_out may be ref: counts are read before any of them is written.)
+  for (int64_t base = 0; base < n_pages; base += kPlanThreads) {
+    const int64_t p = base + tid;
+    if (p < n_pages && p >= live && ref_out != ref) ref_out[p] = 0;
+    if (p < live && ref_out != ref) ref_out[p] = ref[p];
+  }
+  __syncthreads();
+  for (int64_t i = tid; i < n_pages / 2; i += kPlanThreads) {
+    if (i < movers) {
+      const int from = pairs[2 * i], dst = pairs[2 * i + 1];
+      to[from] = dst;
+      ref_out[dst] = ref[from];
+      if (ref_out == ref) ref_out[from] = 0;
+    } else {
+      pairs[2 * i] = -1;
+      pairs[2 * i + 1] = -1;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kListThreads) void compact_table_kernel(
+    const int32_t* table, int64_t stride, int rows, int entries, int32_t* out, int64_t out_stride,
+    int n_pages, const int32_t* __restrict__ to) {
+  const int64_t all = (int64_t)rows * entries;
+  for (int64_t i = (int64_t)blockIdx.x * kListThreads + threadIdx.x; i < all;
+       i += (int64_t)gridDim.x * kListThreads) {
+    const int64_t r = i / entries, e = i - r * entries;
+    const int page = table[r * stride + e];
+    out[r * out_stride + e] = page >= 0 && page < n_pages ? to[page] : page;
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Copy: 16 bytes a thread and step, workgroups over (pair, pool, piece of the page).
+constexpr int kCopyUnroll = 4;
+constexpr int64_t kCopyPiece = 16 * kListThreads * kCopyUnroll;
+
+__global__ __launch_bounds__(kListThreads) void copy_kernel(char* base, int64_t n_pools,
+                                                            int64_t pool_stride, int n_pages,
+                                                            int64_t page_bytes,
+                                                            const int32_t* __restrict__ pairs,
+                                                            int64_t n, const int32_t* n_dev) {
+  const int64_t pieces = (page_bytes + kCopyPiece - 1) / kCopyPiece;
+  const int64_t count = n_dev ? min((int64_t)max(*n_dev, 0), n) : n;
+  const int64_t all = count * n_pools * pieces;
+  for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
+    const int64_t piece = w % pieces, rest = w / pieces;
+    const int64_t pool = rest % n_pools, i = rest / n_pools;
+    const int from = pairs[2 * i], to = pairs[2 * i + 1];
+    if (from < 0 || from >= n_pages || to < 0 || to >= n_pages || from == to) continue;
+    const char* s = base + pool * pool_stride + from * page_bytes;
+    char* d = base + pool * pool_stride + to * page_bytes;
+    v4u x[kCopyUnroll];
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+      const int64_t o = piece * kCopyPiece + 16 * (u * kListThreads + threadIdx.x);
+      if (o < page_bytes) x[u] = *reinterpret_cast<const v4u*>(s + o);
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+      const int64_t o = piece * kCopyPiece + 16 * (u * kListThreads + threadIdx.x);
+      if (o < page_bytes) *reinterpret_cast<v4u*>(d + o) = x[u];
+    }
+  }
+}
+
+aatc_status done() { return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE; }
+
+int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+}  // namespace
+
+aatc_status launch_pages_copy(void* base, int64_t n_pools, int64_t pool_stride, int64_t n_pages,
+                              int64_t page_bytes, const int32_t* pairs, int64_t n,
+                              const int32_t* n_dev, void* stream) {
+  const int64_t pieces = (page_bytes + kCopyPiece - 1) / kCopyPiece;
+  // At most 2^14 workgroups, which then take several pieces each.
+  const int64_t cap = (int64_t)1 << 14;
+  const int64_t grid = n > cap || pieces > cap ? cap : std::min(cap, n * n_pools * pieces);
+  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)grid), dim3(kListThreads), 0,
+                     (hipStream_t)stream, static_cast<char*>(base), n_pools, pool_stride,
+                     (int)n_pages, page_bytes, pairs, n, n_dev);
+  return done();
+}
+
+aatc_status launch_pages_fork(const aatc_page_table& src, const aatc_page_table& dst,
+                              int32_t* ref, int64_t n_pages, const int32_t* pairs, int64_t n,
+                              void* stream) {
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(kListThreads), 0, (hipStream_t)stream,
+                     src.table, src.stride, src.rows, dst.table, dst.stride, dst.rows,
+                     src.max_pages, ref, (int)n_pages, pairs, n);
+  return done();
+}
+
+aatc_status launch_pages_free(const aatc_page_table& t, int32_t* ref, int64_t n_pages,
+                              const int32_t* rows, int64_t n, void* stream) {
+  hipLaunchKernelGGL(free_kernel, dim3((unsigned)n), dim3(kListThreads), 0, (hipStream_t)stream,
+                     t.table, t.stride, t.rows, t.max_pages, ref, (int)n_pages, rows);
+  return done();
+}
+
+size_t pages_workspace_bytes(int64_t rows, int64_t n_pages) {
+  return (size_t)(2 * rows + n_pages) * sizeof(int32_t);
+}
+
+aatc_status launch_pages_reserve(const aatc_page_table& t, int32_t* ref, int64_t n_pages,
+                                 int page_tokens, const int32_t* held, const int32_t* wanted,
+                                 int32_t* pairs, int32_t* lacking, void* workspace, void* stream) {
+  const int64_t most = (int64_t)t.max_pages * page_tokens;
+  const int len_max = (int)std::min<int64_t>(most, INT32_MAX - kMaxPage);
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, (hipStream_t)stream, t.table,
+                     t.stride, t.rows, t.max_pages, ref, (int)n_pages, log2_of(page_tokens),
+                     len_max, held, wanted, pairs, lacking, workspace);
+  return done();
+}
+
+aatc_status launch_pages_compact(const aatc_page_table& t, const int32_t* ref, int64_t n_pages,
+                                 const aatc_page_table& t_out, int32_t* ref_out, int32_t* pairs,
+                                 int32_t* moves, void* workspace, void* stream) {
+  const hipStream_t st = (hipStream_t)stream;
+  auto* to = static_cast<int32_t*>(workspace);
+  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, ref, (int)n_pages,
+                     ref_out, pairs, moves, to);
+  if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
+  const int64_t all = (int64_t)t.rows * t.max_pages;
+  const int64_t grid = std::min<int64_t>((all + kListThreads - 1) / kListThreads, 2048);
+  hipLaunchKernelGGL(compact_table_kernel, dim3((unsigned)grid), dim3(kListThreads), 0, st,
+                     t.table, t.stride, t.rows, t.max_pages, t_out.table, t_out.stride,
+                     (int)n_pages, to);
+  return done();
+}
+
+}  // namespace aatc

@@ -1,0 +1,249 @@
+// Rotary positions, alone and on the way into the pages of a cache.
+//
+// Pair i of a head (channels (i, i + half) or (2 i, 2 i + 1)) at position p is turned by the
+// angle p f_i and scaled:  (a, b) -> factor (a cos - b sin, b cos + a sin);  sign = -1 turns
+// back (the adjoint: the gradient of the forward rotation).  The angle is taken in 64 bits, as
+// revolutions p f_i / 2 pi less the nearest whole number, so that far positions lose nothing;
+// sine and cosine of what is left, the products and their sum are in 32 bits, rounded once to
+// the output's type.
+//
+// Bound by memory: 16-byte loads and stores, a wave to a token and some of its heads, whose
+// sines it computes once (a lane each) while its loads are on their way.
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include "paged.h"
+#include "params.h"
+
+namespace aatc {
+namespace {
+
+constexpr int kTurnThreads = 256;
+constexpr int kTurnWaves = kTurnThreads / 64;
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<AATC_F32> {
+  using type = float;
+  static __device__ float get(float x) { return x; }
+  static __device__ float put(float x) { return x; }
+};
+template <>
+struct Elem<AATC_BF16> {
+  using type = __bf16;
+  static __device__ float get(__bf16 x) { return (float)x; }
+  static __device__ __bf16 put(float x) { return (__bf16)x; }
+};
+template <>
+struct Elem<AATC_F16> {
+  using type = _Float16;
+  static __device__ float get(_Float16 x) { return (float)x; }
+  static __device__ _Float16 put(float x) { return (_Float16)x; }
+};
+
+template <class T, int E>
+struct alignas(sizeof(T) * E < 16 ? sizeof(T) * E : 16) Chunk {
+  T e[E];
+};
+
+// XT: type of the tokens and of q_out, CT: of the pages; INTER: interleaved pairs; VEC: 16-byte
+// aligned rows, and half a multiple of a chunk's elements unless interleaved.
+template <int XD, int CD, bool INTER, bool VEC>
+__global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int heads_per_wave) {
+  using X = Elem<XD>;
+  using C = Elem<CD>;
+  using XT = typename X::type;
+  using CT = typename C::type;
+  __shared__ float2 cs[kTurnWaves][kD / 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t tok = (int64_t)blockIdx.x * kTurnWaves + wave;
+  const bool in = tok < a.n_tok;
+  const int p = in ? a.pos[tok] : 0;
+  const bool on = in && !(a.skip_negative && p < 0);
+  if (on && lane < a.half) {
+    const double rev = (double)p * a.freq[lane] * 0.15915494309189533577;   // 1 / 2 pi
+    float s, c;
+    sincospif((float)(2.0 * (rev - rint(rev))), &s, &c);
+    cs[wave][lane] = make_float2(a.factor * c, a.sign * a.factor * s);
+  }
+  __syncthreads();
+  if (!on) return;
+  // The token's slot in the pages (-1: none).
+  int64_t slot = -1;
+  if (a.heads[1] > 0) {
+    const int64_t row = a.seq ? a.seq[tok] : tok;
+    const int at = p >> a.page_shift;
+    if (row >= 0 && row < a.rows && at < a.max_pages) {
+      const int page = a.table[row * a.table_stride + at];
+      if (page >= 0 && page < a.n_pages)
+        slot = page * a.page_stride + (p & ((1 << a.page_shift) - 1)) * a.tok_stride;
+    }
+  }
+  const int half = a.half, rot = 2 * half;
+  const int turned = a.heads[0] + a.heads[1], all = turned + a.heads[2];
+  const int h_end = min(all, (int)(blockIdx.y + 1) * heads_per_wave);
+  // Source of head h and where it goes: q_out, or a page (null: nowhere).
+  auto source = [&](int h) -> const XT* {
+    const int part = h < a.heads[0] ? 0 : h < turned ? 1 : 2;
+    const int hh = h - (part == 0 ? 0 : part == 1 ? a.heads[0] : turned);
+    return static_cast<const XT*>(a.x[part]) + tok * a.x_stride[part] + hh * kD;
+  };
+  auto q_dest = [&](int h) { return static_cast<XT*>(a.q_out) + tok * a.q_out_stride + h * kD; };
+  auto page_dest = [&](int h) {
+    const int hh = h - (h < turned ? a.heads[0] : turned);
+    return static_cast<CT*>(h < turned ? a.k_pages : a.v_pages) + slot + hh * a.head_stride;
+  };
+  if constexpr (VEC) {
+    constexpr int E = 16 / sizeof(XT);                 // elements of a chunk
+    using XC = Chunk<XT, E>;
+    using CC = Chunk<CT, E>;
+    // Lanes of a head: two chunks each, E apart in the head by 128 / 2, or by `half` for the
+    // pairs of the half layout.
+    constexpr int LH = kD / (2 * E), HW = 64 / LH;     // lanes per head, heads at a time
+    const int sub = lane % LH;
+    for (int h = blockIdx.y * heads_per_wave + lane / LH; h < h_end; h += HW) {
+      const bool to_q = h < a.heads[0], turn = h < turned;
+      if (!to_q && slot < 0) continue;
+      const XT* src = source(h);
+      XT* dq = to_q ? q_dest(h) : nullptr;
+      CT* dc = to_q ? nullptr : page_dest(h);
+      auto store = [&](int c, const float (&y)[E]) {
+        if (to_q) {
+          XC o;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o.e[e] = X::put(y[e]);
+          *reinterpret_cast<XC*>(dq + c) = o;
+        } else {
+          CC o;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o.e[e] = C::put(y[e]);
+          *reinterpret_cast<CC*>(dc + c) = o;
+        }
+      };
+      auto pass = [&](int c) {                         // a chunk that is not turned
+        const XC x = *reinterpret_cast<const XC*>(src + c);
+        if (to_q) {
+          if (a.copy_rest) *reinterpret_cast<XC*>(dq + c) = x;
+          return;
+        }
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = X::get(x.e[e]);
+        store(c, y);
+      };
+      if (!turn) {
+        pass(E * sub);
+        pass(E * (sub + LH));
+      } else if constexpr (INTER) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int c = E * (sub + LH * u);
+          if (c >= rot) {
+            pass(c);
+            continue;
+          }
+          const XC x = *reinterpret_cast<const XC*>(src + c);
+          float y[E];
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const int i = (c + e) / 2;
+            const float2 w = cs[wave][i < half ? i : 0];
+            const float u0 = X::get(x.e[e]), u1 = X::get(x.e[e + 1]);
+            y[e] = i < half ? u0 * w.x - u1 * w.y : u0;
+            y[e + 1] = i < half ? u1 * w.x + u0 * w.y : u1;
+          }
+          store(c, y);
+        }
+      } else {
+        if (E * sub < half) {
+          const int c = E * sub;
+          const XC x0 = *reinterpret_cast<const XC*>(src + c);
+          const XC x1 = *reinterpret_cast<const XC*>(src + half + c);
+          float y0[E], y1[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float2 w = cs[wave][c + e];
+            const float u0 = X::get(x0.e[e]), u1 = X::get(x1.e[e]);
+            y0[e] = u0 * w.x - u1 * w.y;
+            y1[e] = u1 * w.x + u0 * w.y;
+          }
+          store(c, y0);
+          store(half + c, y1);
+        }
+        for (int c = rot + E * sub; c < kD; c += E * LH) pass(c);
+      }
+    }
+  } else {
+    for (int h = blockIdx.y * heads_per_wave; h < h_end; ++h) {
+      const bool to_q = h < a.heads[0], turn = h < turned;
+      if (!to_q && slot < 0) continue;
+      const XT* src = source(h);
+      XT* dq = to_q ? q_dest(h) : nullptr;
+      CT* dc = to_q ? nullptr : page_dest(h);
+      auto put = [&](int c, float y) {
+        if (to_q) dq[c] = X::put(y);
+        else dc[c] = C::put(y);
+      };
+      if (turn && lane < half) {
+        const int c0 = INTER ? 2 * lane : lane, c1 = INTER ? 2 * lane + 1 : lane + half;
+        const float2 w = cs[wave][lane];
+        const float u0 = X::get(src[c0]), u1 = X::get(src[c1]);
+        put(c0, u0 * w.x - u1 * w.y);
+        put(c1, u1 * w.x + u0 * w.y);
+      }
+      for (int c = (turn ? rot : 0) + lane; c < kD; c += 64) {
+        if (!to_q) put(c, X::get(src[c]));
+        else if (a.copy_rest) dq[c] = src[c];
+      }
+    }
+  }
+}
+
+template <int XD, int CD>
+aatc_status launch_turn_types(const TurnArgs& a, int layout, bool vec, hipStream_t st) {
+  const int all = a.heads[0] + a.heads[1] + a.heads[2];
+  const int64_t blocks = (a.n_tok + kTurnWaves - 1) / kTurnWaves;
+  // A wave takes up to 32 heads of its token; with few tokens fewer, so that the chip's compute
+  // units all have some.
+  int per = all < 32 ? all : 32;
+  while (per > 8 && blocks * ((all + per - 1) / per) < 512) per = (per + 1) / 2;
+  const dim3 grid((unsigned)blocks, (unsigned)((all + per - 1) / per));
+  const bool inter = layout == AATC_ROPE_INTERLEAVED;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kTurnThreads), 0, st, a, per);
+  };
+  if (vec) inter ? launch(turn_kernel<XD, CD, true, true>) : launch(turn_kernel<XD, CD, false, true>);
+  else inter ? launch(turn_kernel<XD, CD, true, false>) : launch(turn_kernel<XD, CD, false, false>);
+  return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
+}
+
+template <int XD>
+aatc_status launch_turn_x(const TurnArgs& a, aatc_dtype c, int layout, bool vec, hipStream_t st) {
+  switch (c) {
+    case AATC_F32: return launch_turn_types<XD, AATC_F32>(a, layout, vec, st);
+    case AATC_BF16: return launch_turn_types<XD, AATC_BF16>(a, layout, vec, st);
+    default: return launch_turn_types<XD, AATC_F16>(a, layout, vec, st);
+  }
+}
+
+}  // namespace
+
+aatc_status launch_turn(const TurnArgs& a, aatc_dtype x_dtype, aatc_dtype c_dtype, int layout,
+                        void* stream) {
+  const int size = x_dtype == AATC_F32 ? 4 : 2, e = 16 / size;
+  bool vec = layout == AATC_ROPE_INTERLEAVED || a.half % e == 0;
+  for (int i = 0; i < 3; ++i)
+    if (a.heads[i] > 0)
+      vec = vec && reinterpret_cast<uintptr_t>(a.x[i]) % 16 == 0 && a.x_stride[i] % e == 0;
+  if (a.heads[0] > 0)
+    vec = vec && reinterpret_cast<uintptr_t>(a.q_out) % 16 == 0 && a.q_out_stride % e == 0;
+  const hipStream_t st = (hipStream_t)stream;
+  switch (x_dtype) {
+    case AATC_F32: return launch_turn_x<AATC_F32>(a, c_dtype, layout, vec, st);
+    case AATC_BF16: return launch_turn_x<AATC_BF16>(a, c_dtype, layout, vec, st);
+    default: return launch_turn_x<AATC_F16>(a, c_dtype, layout, vec, st);
+  }
+}
+
+}  // namespace aatc
