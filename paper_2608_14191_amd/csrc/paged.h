@@ -56,7 +56,7 @@ struct PagedArgs {
   Partial* seg;                   // [batch][n_q_heads] softmax partials instead of outputs
   const float* slopes;            // [n_q_heads] or null
   unsigned* counters;
-  float* parts;
+  Partial* parts;
   int batch, n_q_heads, n_kv_heads, G, hg, q_dtype;
   int n_pages, max_pages, page_shift, len_max;    // len_max: tokens that a row can name
   int window, sink;

@@ -31,16 +31,18 @@
 namespace aatc {
 namespace {
 
-constexpr int kPagedThreads = 256, kPagedWaves = kPagedThreads / 64;
-constexpr int kPagedGroups = 512;                 // most workgroups: two per compute unit
+constexpr int kPagedThreads = 512, kPagedWaves = kPagedThreads / 64;
+constexpr int kPagedGroups = 256;                 // most workgroups: one per compute unit
 constexpr int kPagedHeads = 16;                   // query heads of a row
-constexpr int kQuotaMin = kPagedWaves;            // tiles of a workgroup: one per wave at least
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kPartFloats = kPagedHeads * (kD + 2);   // m [16], l [16], o [16][128]
+constexpr int kPartsBytes = 2 * kPagedGroups * kPagedHeads * (int)sizeof(Partial);
 constexpr int kRowStride = 64;                    // counters 256 bytes apart (their atomics
                                                   // would queue on one cache line)
+constexpr int kRsrcWord3 = 0x00020000;            // raw buffer descriptor word 3 (gfx950)
+constexpr int kCoherent = 16;                     // cache policy sc1: device-coherent access
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -57,17 +59,6 @@ __device__ inline float over_groups_sum(float v) {
   v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Stores and loads of workspace that other workgroups write: performed where every compute
-// unit of the device sees them.
-__device__ inline void st_dev(float* p, float v) {
-  __hip_atomic_store(reinterpret_cast<unsigned*>(p), __float_as_uint(v), __ATOMIC_RELAXED,
-                     __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ inline float ld_dev(const float* p) {
-  return __uint_as_float(__hip_atomic_load(reinterpret_cast<const unsigned*>(p), __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_AGENT));
 }
 
 // N consecutive query elements from element i on (aligned to the element only).
@@ -291,13 +282,111 @@ struct Full32 {
   }
 };
 
+// tanh to a few ulps: for small |x| the first terms of its odd series (the next is below 2^-25 of
+// x at 0.55), else from exp(-2 |x|).
+__device__ inline float tanh_of(float x) {
+  const float y = fabsf(x), s = y * y;
+  float r = 0.0014558343f;                         // 21844 / 6081075, -1382 / 155925, ...
+  r = fmaf(-r, s, 0.003592128f);
+  r = fmaf(-r, s, 0.0088632356f);
+  r = fmaf(-r, s, 0.021869488f);
+  r = fmaf(-r, s, 0.053968254f);
+  r = fmaf(-r, s, 0.13333334f);
+  r = fmaf(-r, s, 0.33333334f);
+  const float small = fmaf(-r * s, y, y);
+  const float e = __builtin_amdgcn_exp2f(-2.f * kLog2e * y);
+  const float large = (1.f - e) / (1.f + e);
+  return copysignf(y < 0.55f ? small : large, x);
+}
+
+// A workgroup's parts of one row.  LDS of the joins: the waves' sums, then (the same bytes) the
+// weights of a row's parts and the sums over groups of them.
+struct JoinSpace {
+  union {
+    float sums[kPagedWaves][kPagedHeads][kD + 4];  // (rows padded: banks)
+    struct {
+      float m[kPagedHeads][kPagedGroups], l[kPagedHeads][kPagedGroups];
+    } parts;
+  };
+  v4f groups[kPagedThreads];
+  float m[kPagedWaves][kPagedHeads], l[kPagedWaves][kPagedHeads];
+  float top[kPagedHeads], total[kPagedHeads];
+};
+
+// Joins the parts of a row, written by the workgroups from `first` on, in their order: weights
+// first (a wave to a head), then the sums, 16 bytes a load, whose first loads are on their way
+// meanwhile.
+template <class Finish, class Slot>
+__device__ inline void join_parts(JoinSpace& sh, int parts, int first, int heads, Finish finish,
+                                  Slot slot) {
+  constexpr int U = 8;                             // loads in flight
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int units = heads * (kD / 4), groups = kPagedThreads / units;
+  const int unit = tid % units, grp = tid / units, h = unit / (kD / 4), c4 = unit % (kD / 4);
+  const bool on = grp < groups;
+  v4f x[U];
+  auto issue = [&](int p0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * groups;
+      x[u] = (on & (p < parts)) ? slot(first + p, h, 16 + 16 * c4) : (v4f){0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  issue(grp);
+  for (int i = tid; i < heads * parts; i += kPagedThreads) {
+    const int hh = i % heads, p = i / heads;
+    const v4f ml = slot(first + p, hh, 0);
+    sh.parts.m[hh][p] = ml[0];
+    sh.parts.l[hh][p] = ml[1];
+  }
+  __syncthreads();
+  for (int hh = wave; hh < heads; hh += kPagedWaves) {
+    float m = -INFINITY, l = 0.f;
+    for (int p = lane; p < parts; p += 64)
+      if (sh.parts.l[hh][p] != 0.f) m = fmaxf(m, sh.parts.m[hh][p]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int p = lane; p < parts; p += 64) {
+      const float pl = sh.parts.l[hh][p];
+      const float w = pl == 0.f ? 0.f : __builtin_amdgcn_exp2f(sh.parts.m[hh][p] - ref);
+      l += pl == 0.f ? 0.f : w * pl;               // (NaN stays)
+      sh.parts.m[hh][p] = w;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+    if (lane == 0) {
+      sh.top[hh] = m;
+      sh.total[hh] = l;
+    }
+  }
+  __syncthreads();
+  v4f acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = grp;;) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * groups;
+      const float w = (on & (p < parts)) ? sh.parts.m[h][p] : 0.f;
+      acc += w * x[u];
+    }
+    p0 += U * groups;
+    if (p0 - grp >= parts) break;
+    issue(p0);
+  }
+  sh.groups[tid] = acc;
+  __syncthreads();
+  if (tid < units) {
+    for (int q = 1; q < groups; ++q) acc += sh.groups[q * units + tid];
+    finish(h, c4, sh.top[h], sh.total[h], acc);
+  }
+}
+
 template <class M, int QT>
 __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
   constexpr int TT = M::kTokens, NM = M::kMine;
-  constexpr int kOs = kD + 4;                      // LDS row of a head's sums (banks)
-  __shared__ float so[kPagedWaves][kPagedHeads][kOs];
-  __shared__ float sm[kPagedWaves][kPagedHeads], sl[kPagedWaves][kPagedHeads];
-  __shared__ int scan[kPagedWaves], found[2];
+  __shared__ JoinSpace sh;
+  __shared__ int scan[2][kPagedWaves], found[2];
   __shared__ unsigned arrived;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -308,46 +397,81 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
     return row_tiles(len, a.window, a.sink, TT);
   };
 
-  // The line: every thread adds up a run of sequences, a scan over the workgroup.
+  // Where this workgroup begins: sequence, its first tile in the line, the row and its first tile.
+  int seq, row, start, quota, begin, end;
+  RowTiles rt;
+  // The batch's tiles and longest row.
+  int total, longest, mine = 0, incl = 0;
   const int each = (a.batch + kPagedThreads - 1) / kPagedThreads;
   const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += tiles_of(b).n * rows;
-  int incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(incl, o, 64);
-    incl += lane >= o ? up : 0;
-  }
-  if (lane == 63) scan[wave] = incl;
-  __syncthreads();
-  int total = 0;
-#pragma unroll
-  for (int w = 0; w < kPagedWaves; ++w) {
-    incl += w < wave ? scan[w] : 0;
-    total += scan[w];
-  }
-  const int quota = max(kQuotaMin, (total + (int)gridDim.x - 1) / (int)gridDim.x);
-  const int begin = (int)blockIdx.x * quota;
-  if (begin >= total) return;                      // (uniform)
-  const int end = min(begin + quota, total);
-  int at = incl - mine;
-  if (begin >= at && begin < incl) {               // (one thread: runs without tiles are empty)
-    int b = b0;
-    for (;; ++b) {
-      const int t = tiles_of(b).n * rows;
-      if (begin < at + t) break;
-      at += t;
+  if (a.batch == 1) {
+    longest = tiles_of(0).n;
+    total = longest * rows;
+  } else {
+    // Every thread adds up a run of sequences, a scan over the workgroup.
+    longest = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int t = tiles_of(b).n;
+      mine += t * rows;
+      longest = max(longest, t);
     }
-    found[0] = b;
-    found[1] = at;
+    incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(incl, o, 64);
+      incl += lane >= o ? up : 0;
+      longest = max(longest, __shfl_xor(longest, o, 64));
+    }
+    if (lane == 63) {
+      scan[0][wave] = incl;
+      scan[1][wave] = longest;
+    }
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) {
+      incl += w < wave ? scan[0][w] : 0;
+      total += scan[0][w];
+      longest = max(longest, scan[1][w]);
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    longest = __builtin_amdgcn_readfirstlane(longest);
   }
-  __syncthreads();
-  int seq = __builtin_amdgcn_readfirstlane(found[0]);
-  const int before = __builtin_amdgcn_readfirstlane(found[1]);
-  RowTiles rt = tiles_of(seq);
-  int row = (begin - before) / rt.n;               // of the sequence
-  int start = before + row * rt.n;               // the row's first tile in the line
+  if (rows_whole(longest, a.batch * rows, (int)gridDim.x)) {
+    if ((int)blockIdx.x >= a.batch * rows) return; // (uniform)
+    seq = (int)blockIdx.x / rows;
+    row = (int)blockIdx.x % rows;
+    rt = tiles_of(seq);
+    quota = longest;
+    begin = start = (int)blockIdx.x * quota;
+    end = begin + rt.n;
+  } else {
+    quota = quota_of(total, (int)gridDim.x);
+    begin = (int)blockIdx.x * quota;
+    if (begin >= total) return;                    // (uniform)
+    end = min(begin + quota, total);
+    int before = 0;
+    seq = 0;
+    if (a.batch > 1) {
+      int at = incl - mine;
+      if (begin >= at && begin < incl) {           // (one thread: runs without tiles are empty)
+        int b = b0;
+        for (;; ++b) {
+          const int t = tiles_of(b).n * rows;
+          if (begin < at + t) break;
+          at += t;
+        }
+        found[0] = b;
+        found[1] = at;
+      }
+      __syncthreads();
+      seq = __builtin_amdgcn_readfirstlane(found[0]);
+      before = __builtin_amdgcn_readfirstlane(found[1]);
+    }
+    rt = tiles_of(seq);
+    row = (begin - before) / rt.n;
+    start = before + row * rt.n;
+  }
 
   for (;;) {
     const int len = min(max(a.seq_len[seq], 0), a.len_max);
@@ -360,6 +484,27 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
     const char* kb = a.k + kvh * a.head_stride;
     const char* vb = a.v + kvh * a.head_stride;
 
+    // Page of the 8-token block `blk` of the tile at token t0 (-1: none there).
+    auto page_of = [&](int t0, int blk) {
+      const int i = (t0 + 8 * blk) >> a.page_shift;
+      return i < a.max_pages ? table[i] : -1;
+    };
+    auto exists = [&](int page) { return (page >= 0) & (page < a.n_pages); };
+    const int slot_mask = (1 << a.page_shift) - 1;
+    auto key_row = [&](int t0, int page) {
+      const int t = t0 + M::key_token(0, n);
+      return kb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
+    };
+    auto value_row = [&](int t0, int page) {
+      const int t = t0 + NM * g;
+      return vb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
+    };
+
+    // Two tiles ahead: pages; one tile ahead: keys and values.
+    int i = first + wave;
+    int t0 = rt.token(min(i, last - 1), TT), t1 = rt.token(min(i + kPagedWaves, last - 1), TT);
+    int kp = page_of(t0, M::key_block(n)), vp = page_of(t0, M::value_block(g));
+    int kp1 = page_of(t1, M::key_block(n)), vp1 = page_of(t1, M::value_block(g));
     typename M::template Query<QT> q;
     q.load(a.q, a.q_dtype, (int64_t)seq * a.q_stride + (int64_t)(h0 + min(n, heads - 1)) * kD,
            n < heads, g);
@@ -369,49 +514,23 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
     v4f acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
-
-    // Page of the 8-token block `blk` of the tile at token t0 (-1: none there).
-    auto page_of = [&](int t0, int blk) {
-      const int i = (t0 + 8 * blk) >> a.page_shift;
-      return i < a.max_pages ? table[i] : -1;
-    };
-    const int slot_mask = (1 << a.page_shift) - 1;
-    auto key_row = [&](int t0, int page) {
-      const int t = t0 + M::key_token(0, n);
-      return kb + max(page, 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
-    };
-    auto value_row = [&](int t0, int page) {
-      const int t = t0 + NM * g;
-      return vb + max(page, 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
-    };
-    auto checked = [&](int page) { return page >= 0 && page < a.n_pages ? page : -1; };
-
     typename M::Keys key;
     typename M::Values val;
-    int i = first + wave;
-    int t0 = 0, vp = -1;
     if (i < last) {
-      t0 = rt.token(i, TT);
-      const int kp = checked(page_of(t0, M::key_block(n)));
-      vp = checked(page_of(t0, M::value_block(g)));
       key.load(key_row(t0, kp), a.tok_stride, g);
       val.load(value_row(t0, vp), a.tok_stride, n);
     }
-    while (i < last) {
-      const int in = i + kPagedWaves;
-      const bool more = in < last;
-      const int tn = more ? rt.token(in, TT) : t0;
-      int kpn = -1, vpn = -1;
-      if (more) {
-        kpn = checked(page_of(tn, M::key_block(n)));
-        vpn = checked(page_of(tn, M::value_block(g)));
-      }
+    for (; i < last; i += kPagedWaves) {
+      const bool more = i + kPagedWaves < last;
       float z[NM];
       M::template scores<QT>(key, q, z);
-      if (more) key.load(key_row(tn, kpn), a.tok_stride, g);
+      if (more) key.load(key_row(t1, kp1), a.tok_stride, g);
+      const int t2 = rt.token(min(i + 2 * kPagedWaves, last - 1), TT);
+      const int kp2 = page_of(t2, M::key_block(n)), vp2 = page_of(t2, M::value_block(g));
       if (a.cap > 0.f) {
+        const float in = a.scale / a.cap, out = a.cap * kLog2e;
 #pragma unroll
-        for (int e = 0; e < NM; ++e) z[e] = a.cap * tanhf(z[e] * a.scale / a.cap) * kLog2e;
+        for (int e = 0; e < NM; ++e) z[e] = out * tanh_of(z[e] * in);
       } else {
 #pragma unroll
         for (int e = 0; e < NM; ++e) z[e] *= a.scale * kLog2e;
@@ -421,14 +540,15 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
         for (int e = 0; e < NM; ++e) z[e] -= slope * (float)(len - 1 - (t0 + NM * g + e));
       }
       // A tile that is attended as a whole needs no masks.
+      const bool there = exists(vp);
       const bool whole = t0 + TT <= len && (t0 >= lo || t0 + TT <= a.sink) &&
-                         __builtin_amdgcn_ballot_w64(vp < 0) == 0;
+                         __builtin_amdgcn_ballot_w64(!there) == 0;
       if (!whole) {
 #pragma unroll
         for (int e = 0; e < NM; ++e) {
           const int t = t0 + NM * g + e;
           // (no short circuits: selects, not branches)
-          const bool on = (vp >= 0) & (t < len) & ((t >= lo) | (t < a.sink));
+          const bool on = there & (t < len) & ((t >= lo) | (t < a.sink));
           z[e] = on ? z[e] : -INFINITY;
           val.keep(e, on);
         }
@@ -450,62 +570,67 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] *= sa;
       M::accumulate(val, p, acc);
-      if (more) val.load(value_row(tn, vpn), a.tok_stride, n);
-      i = in;
-      t0 = tn;
-      vp = vpn;
+      if (more) val.load(value_row(t1, vp1), a.tok_stride, n);
+      t0 = t1, vp = vp1;
+      t1 = t2, kp1 = kp2, vp1 = vp2;
     }
     l_run = over_groups_sum(l_run);
 
     // The waves' parts meet in LDS.
     if (g == 0) {
-      sm[wave][n] = m_run;
-      sl[wave][n] = l_run;
+      sh.m[wave][n] = m_run;
+      sh.l[wave][n] = l_run;
     }
+    if (n < heads) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) so[wave][n][M::channel(j, r, g)] = acc[j][r];
+        for (int r = 0; r < 4; ++r) sh.sums[wave][n][M::channel(j, r, g)] = acc[j][r];
+    }
     __syncthreads();
 
     const RowShare share = row_share(start, rt.n, quota);
     const int parts = share.last - share.first + 1;
     // What a row ends as: outputs and log-sum-exp, or a partial for another join.
-    auto finish = [&](int h, int c, float mm, float l, float o) {
+    auto finish = [&](int h, int c4, float m, float l, v4f o) {
       if (a.seg) {
         Partial* s = a.seg + q_row + h;
-        s->o[c] = o;
-        if (c == 0) {
-          s->m = mm;
-          s->l = l;
-        }
+        reinterpret_cast<v4f*>(s->o)[c4] = o;
+        if (c4 == 0) *reinterpret_cast<v4f*>(s) = (v4f){m, l, 0.f, 0.f};
         return;
       }
-      a.out[(q_row + h) * kD + c] = l == 0.f ? 0.f : o / l;
-      if (a.lse && c == 0) a.lse[q_row + h] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+      const v4f zero = {0.f, 0.f, 0.f, 0.f};
+      reinterpret_cast<v4f*>(a.out)[(q_row + h) * (kD / 4) + c4] = l == 0.f ? zero : o / l;
+      if (a.lse && c4 == 0) a.lse[q_row + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     };
-    float* slots = a.parts;
-    for (int x = tid; x < heads * kD; x += kPagedThreads) {
-      const int h = x / kD, c = x % kD;
-      float mm = sm[0][h];
+    // Part slots: Partial [kPagedHeads], stored and loaded where every compute unit sees them.
+    const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, kPartsBytes, kRsrcWord3);
+    auto part_at = [&](int w, int h) {
+      return (part_slot(w, start, quota) * kPagedHeads + h) * (int)sizeof(Partial);
+    };
+    const int units = heads * (kD / 4);            // (head, four channels)
+    for (int x = tid; x < units; x += kPagedThreads) {
+      const int h = x / (kD / 4), c4 = x % (kD / 4);
+      float m = sh.m[0][h];
 #pragma unroll
-      for (int w = 1; w < kPagedWaves; ++w) mm = fmaxf(mm, sm[w][h]);
-      float l = 0.f, o = 0.f;
+      for (int w = 1; w < kPagedWaves; ++w) m = fmaxf(m, sh.m[w][h]);
+      float l = 0.f;
+      v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kPagedWaves; ++w) {
-        const float f = sm[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][h] - mm);
-        l += sl[w][h] == 0.f ? 0.f : f * sl[w][h];
-        o += f == 0.f ? 0.f : f * so[w][h][c];
+        const float f = sh.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[w][h] - m);
+        l += sh.l[w][h] == 0.f ? 0.f : f * sh.l[w][h];
+        const v4f s = *reinterpret_cast<const v4f*>(&sh.sums[w][h][4 * c4]);
+        o += f * s;
       }
       if (parts == 1) {
-        finish(h, c, mm, l, o);
+        finish(h, c4, m, l, o);
       } else {
-        float* slot = slots + (int64_t)part_slot(blockIdx.x, start, quota) * kPartFloats;
-        st_dev(slot + 2 * kPagedHeads + h * kD + c, o);
-        if (c == 0) {
-          st_dev(slot + h, mm);
-          st_dev(slot + kPagedHeads + h, l);
-        }
+        const int off = part_at(blockIdx.x, h);
+        __builtin_amdgcn_raw_buffer_store_b128((v4i)o, slots, off + 16 + 16 * c4, 0, kCoherent);
+        if (c4 == 0)
+          __builtin_amdgcn_raw_buffer_store_b128((v4i)(v4f){m, l, 0.f, 0.f}, slots, off, 0,
+                                                 kCoherent);
       }
     }
     if (parts > 1) {
@@ -516,23 +641,10 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
         arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (arrived == (unsigned)parts - 1u) {
-        for (int x = tid; x < heads * kD; x += kPagedThreads) {
-          const int h = x / kD, c = x % kD;
-          float mm = -INFINITY, l = 0.f, o = 0.f;
-          for (int w = share.first; w <= share.last; ++w) {
-            const float* slot = slots + (int64_t)part_slot(w, start, quota) * kPartFloats;
-            const float pm = ld_dev(slot + h), pl = ld_dev(slot + kPagedHeads + h);
-            const float po = ld_dev(slot + 2 * kPagedHeads + h * kD + c);
-            if (pl == 0.f) continue;               // no attended token there
-            const float nm = fmaxf(mm, pm);
-            const float ref = nm == -INFINITY ? 0.f : nm;
-            const float fa = __builtin_amdgcn_exp2f(mm - ref), fb = __builtin_amdgcn_exp2f(pm - ref);
-            l = l * fa + pl * fb;
-            o = o * fa + po * fb;
-            mm = nm;
-          }
-          finish(h, c, mm, l, o);
-        }
+        join_parts(sh, parts, share.first, heads, finish, [&](int w, int h, int off) {
+          return (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, part_at(w, h) + off, 0,
+                                                            kCoherent);
+        });
         if (tid == 0) *counter = 0u;               // as the next call expects it
       }
     }
@@ -555,19 +667,18 @@ size_t counters_bytes(int batch, int n_q_heads, int n_kv_heads) {
 }  // namespace
 
 size_t paged_workspace_bytes(int batch, int n_q_heads, int n_kv_heads) {
-  return counters_bytes(batch, n_q_heads, n_kv_heads) +
-         2 * (size_t)kPagedGroups * kPartFloats * sizeof(float);
+  return counters_bytes(batch, n_q_heads, n_kv_heads) + kPartsBytes;
 }
 
 aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
   a.counters = static_cast<unsigned*>(workspace);
-  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) +
-                                     counters_bytes(a.batch, a.n_q_heads, a.n_kv_heads));
+  a.parts = reinterpret_cast<Partial*>(static_cast<char*>(workspace) +
+                                       counters_bytes(a.batch, a.n_q_heads, a.n_kv_heads));
   const int tt = c_dtype == AATC_F32 ? Full32::kTokens : Half16<__bf16>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
   if (most > (1 << 30)) return AATC_E_UNSUPPORTED;
-  const int grid = (int)std::min<int64_t>(kPagedGroups, (most + kQuotaMin - 1) / kQuotaMin);
+  const int grid = (int)std::min<int64_t>(kPagedGroups, most);
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kPagedThreads), 0, st, a);

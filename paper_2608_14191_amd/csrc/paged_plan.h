@@ -34,6 +34,20 @@ AATC_PAGED_HD inline RowTiles row_tiles(int len, int window, int sink, int tt) {
   return r;
 }
 
+// Rows so short that one workgroup has each in a few rounds of its waves are not shared, if there
+// is a workgroup for every row.
+constexpr int kWholeRow = 32;
+AATC_PAGED_HD inline bool rows_whole(int longest, int rows, int grid) {
+  return longest <= kWholeRow && rows <= grid;
+}
+
+// Else: tiles of a workgroup, one for each of its waves at least.
+constexpr int kQuotaMin = 8;
+AATC_PAGED_HD inline int quota_of(int total, int grid) {
+  const int even = (total + grid - 1) / grid;
+  return even > kQuotaMin ? even : kQuotaMin;
+}
+
 // The tiles of all rows lie in one line, row after row; workgroup w takes those from w quota on.
 // A row that starts at `start` with n tiles is shared by the workgroups first .. last.
 struct RowShare {
