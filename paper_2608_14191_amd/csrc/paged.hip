@@ -23,6 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 #include "paged_plan.h"
@@ -31,11 +32,16 @@
 namespace aatc {
 namespace {
 
-constexpr int kPagedThreads = 512, kPagedWaves = kPagedThreads / 64;
-constexpr int kPagedGroups = 256;                 // most workgroups: one per compute unit
+// Runs (few rows): eight waves a workgroup, one workgroup a compute unit, so that a row has few
+// parts to join (1 x 32768 tokens, 8 KV heads: 31.2 us, with four waves and twice as many 34.0).
+// Lines (many rows): four waves, two workgroups a compute unit, whose row changes cover each
+// other (48 x 2052 tokens, 8 KV heads, float32: 144.5 us, with eight waves 159.9).
+constexpr int kRunWaves = 8, kRunGroups = 256;
+constexpr int kLineWaves = 4, kLineGroups = 512;
+constexpr int kMaxRunRows = 128;                  // two sequences a lane (every row counts one)
 constexpr int kPagedHeads = 16;                   // query heads of a row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kPartsBytes = 2 * kPagedGroups * kPagedHeads * (int)sizeof(Partial);
+constexpr int kPartsBytes = 2 * kLineGroups * kPagedHeads * (int)sizeof(Partial);
 constexpr int kRowStride = 64;                    // counters 256 bytes apart (their atomics
                                                   // would queue on one cache line)
 constexpr int kRsrcWord3 = 0x00020000;            // raw buffer descriptor word 3 (gfx950)
@@ -299,123 +305,177 @@ __device__ inline float tanh_of(float x) {
   return copysignf(y < 0.55f ? small : large, x);
 }
 
-// A workgroup's parts of one row.  LDS of the joins: the waves' sums, then (the same bytes) the
-// weights of a row's parts and the sums over groups of them.
+// LDS of the joins: the waves' sums, then (the same bytes) the weights of a row's parts; and the
+// sums over groups of them.
+template <int W, int GROUPS>
 struct JoinSpace {
   union {
-    float sums[kPagedWaves][kPagedHeads][kD + 4];  // (rows padded: banks)
+    float sums[W][kPagedHeads][kD + 4];            // (rows padded: banks)
     struct {
-      float m[kPagedHeads][kPagedGroups], l[kPagedHeads][kPagedGroups];
+      float m[kPagedHeads][GROUPS], l[kPagedHeads][GROUPS];
     } parts;
   };
-  v4f groups[kPagedThreads];
-  float m[kPagedWaves][kPagedHeads], l[kPagedWaves][kPagedHeads];
+  v4f groups[64 * W];
+  float m[W][kPagedHeads], l[W][kPagedHeads];
   float top[kPagedHeads], total[kPagedHeads];
 };
 
-// Joins the parts of a row, written by the workgroups from `first` on, in their order: weights
-// first (a wave to a head), then the sums, 16 bytes a load, whose first loads are on their way
-// meanwhile.
-template <class Finish, class Slot>
-__device__ inline void join_parts(JoinSpace& sh, int parts, int first, int heads, Finish finish,
+// Joins the parts of a row in their order (slot(p, h, offset): 16 bytes of part p of head h):
+// weights first, a wave to a head, then the sums of (head, four channels) units by groups of
+// threads, whose first loads are on their way meanwhile.
+template <int W, int GROUPS, class Finish, class Slot>
+__device__ inline void join_parts(JoinSpace<W, GROUPS>& sh, int parts, int heads, Finish finish,
                                   Slot slot) {
-  constexpr int U = 8;                             // loads in flight
+  constexpr int NT = 64 * W, U = 8;                // U loads in flight
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int units = heads * (kD / 4), groups = kPagedThreads / units;
-  const int unit = tid % units, grp = tid / units, h = unit / (kD / 4), c4 = unit % (kD / 4);
-  const bool on = grp < groups;
+  const int units = heads * (kD / 4);
   v4f x[U];
+  int width = min(units, NT), groups = NT / width;
+  int unit = tid % width, grp = tid / width;
   auto issue = [&](int p0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int p = p0 + u * groups;
-      x[u] = (on & (p < parts)) ? slot(first + p, h, 16 + 16 * c4) : (v4f){0.f, 0.f, 0.f, 0.f};
+      x[u] = ((grp < groups) & (p < parts)) ? slot(p, unit / (kD / 4), 16 + 16 * (unit % (kD / 4)))
+                                            : (v4f){0.f, 0.f, 0.f, 0.f};
     }
   };
   issue(grp);
-  for (int i = tid; i < heads * parts; i += kPagedThreads) {
-    const int hh = i % heads, p = i / heads;
-    const v4f ml = slot(first + p, hh, 0);
-    sh.parts.m[hh][p] = ml[0];
-    sh.parts.l[hh][p] = ml[1];
+  for (int i = tid; i < heads * parts; i += NT) {
+    const int h = i % heads, p = i / heads;
+    const v4f ml = slot(p, h, 0);
+    sh.parts.m[h][p] = ml[0];
+    sh.parts.l[h][p] = ml[1];
   }
   __syncthreads();
-  for (int hh = wave; hh < heads; hh += kPagedWaves) {
+  for (int h = wave; h < heads; h += W) {
     float m = -INFINITY, l = 0.f;
     for (int p = lane; p < parts; p += 64)
-      if (sh.parts.l[hh][p] != 0.f) m = fmaxf(m, sh.parts.m[hh][p]);
+      if (sh.parts.l[h][p] != 0.f) m = fmaxf(m, sh.parts.m[h][p]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     const float ref = m == -INFINITY ? 0.f : m;
     for (int p = lane; p < parts; p += 64) {
-      const float pl = sh.parts.l[hh][p];
-      const float w = pl == 0.f ? 0.f : __builtin_amdgcn_exp2f(sh.parts.m[hh][p] - ref);
+      const float pl = sh.parts.l[h][p];
+      const float w = pl == 0.f ? 0.f : __builtin_amdgcn_exp2f(sh.parts.m[h][p] - ref);
       l += pl == 0.f ? 0.f : w * pl;               // (NaN stays)
-      sh.parts.m[hh][p] = w;
+      sh.parts.m[h][p] = w;
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
     if (lane == 0) {
-      sh.top[hh] = m;
-      sh.total[hh] = l;
+      sh.top[h] = m;
+      sh.total[h] = l;
     }
   }
   __syncthreads();
-  v4f acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = grp;;) {
+  for (int base = 0;;) {
+    const int h = unit / (kD / 4);
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = grp;;) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = p0 + u * groups;
-      const float w = (on & (p < parts)) ? sh.parts.m[h][p] : 0.f;
-      acc += w * x[u];
+      for (int u = 0; u < U; ++u) {
+        const int p = p0 + u * groups;
+        const float w = ((grp < groups) & (p < parts)) ? sh.parts.m[h][p] : 0.f;
+        acc += w * x[u];
+      }
+      p0 += U * groups;
+      if (p0 - grp >= parts) break;                // (uniform)
+      issue(p0);
     }
-    p0 += U * groups;
-    if (p0 - grp >= parts) break;
-    issue(p0);
-  }
-  sh.groups[tid] = acc;
-  __syncthreads();
-  if (tid < units) {
-    for (int q = 1; q < groups; ++q) acc += sh.groups[q * units + tid];
-    finish(h, c4, sh.top[h], sh.total[h], acc);
+    sh.groups[tid] = acc;
+    __syncthreads();
+    if (tid < width) {
+      for (int q = 1; q < groups; ++q) acc += sh.groups[q * width + tid];
+      finish(h, unit % (kD / 4), sh.top[h], sh.total[h], acc);
+    }
+    base += width;
+    if (base >= units) break;                      // (uniform)
+    __syncthreads();
+    width = min(units - base, NT);
+    groups = NT / width;
+    unit = base + tid % width;
+    grp = tid / width;
+    issue(grp);
   }
 }
 
-template <class M, int QT>
-__global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
+template <class M, int QT, bool RUNS>
+__global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged_kernel(PagedArgs a) {
+  constexpr int W = RUNS ? kRunWaves : kLineWaves, NT = 64 * W;
   constexpr int TT = M::kTokens, NM = M::kMine;
-  __shared__ JoinSpace sh;
-  __shared__ int scan[2][kPagedWaves], found[2];
+  __shared__ JoinSpace<W, RUNS ? kRunGroups : kLineGroups> sh;
+  __shared__ int scan[2][W], found[2];
   __shared__ unsigned arrived;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int block = (int)blockIdx.x, grid = (int)gridDim.x;
   const int rows = a.n_kv_heads * a.hg;            // of a sequence
 
-  auto tiles_of = [&](int b) {
-    const int len = min(max(a.seq_len[b], 0), a.len_max);
-    return row_tiles(len, a.window, a.sink, TT);
-  };
+  auto length = [&](int b) { return min(max(a.seq_len[b], 0), a.len_max); };
+  auto tiles_of = [&](int b) { return row_tiles(length(b), a.window, a.sink, TT); };
 
-  // Where this workgroup begins: sequence, its first tile in the line, the row and its first tile.
-  int seq, row, start, quota, begin, end;
+  // This workgroup's share: tiles first .. last - 1 of row `row` of sequence `seq`, part `part` of
+  // `parts`.  Lines: the row begins at tile `start` of the line, the share ends at `end`.
+  int seq = 0, row = 0, first, last, part = 0, parts = 1;
+  int quota = 0, start = 0, end = 0;
   RowTiles rt;
-  // The batch's tiles and longest row.
-  int total, longest, mine = 0, incl = 0;
-  const int each = (a.batch + kPagedThreads - 1) / kPagedThreads;
-  const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
-  if (a.batch == 1) {
-    longest = tiles_of(0).n;
-    total = longest * rows;
+  if constexpr (RUNS) {
+    const int all = a.batch * rows;
+    if (a.batch == 1) {
+      rt = tiles_of(0);
+      parts = runs_of(rt.n, W * smallest_rounds(rt.n * rows, rows, grid, W, [&](int q) {
+                        return rows * runs_of(rt.n, q);
+                      }));
+      row = block / parts;
+      part = block % parts;
+      if (row >= rows) return;                     // (uniform)
+    } else {
+      // Two sequences a lane; every wave does the same.
+      const int n0 = lane < a.batch ? tiles_of(lane).n : 0;
+      const int n1 = lane + 64 < a.batch ? tiles_of(lane + 64).n : 0;
+      auto sum_of = [&](int v) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+        return __builtin_amdgcn_readfirstlane(v);
+      };
+      const int q = W * smallest_rounds(sum_of(n0 + n1) * rows, all, grid, W, [&](int x) {
+                      return rows * sum_of(runs_of(n0, x) + runs_of(n1, x));
+                    });
+      const int r0 = rows * runs_of(n0, q), r1 = rows * runs_of(n1, q);
+      int i0 = r0, i1 = r1;                        // inclusive sums in the sequences' order
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u0 = __shfl_up(i0, o, 64), u1 = __shfl_up(i1, o, 64);
+        i0 += lane >= o ? u0 : 0;
+        i1 += lane >= o ? u1 : 0;
+      }
+      i1 += __shfl(i0, 63, 64);
+      if (block >= __builtin_amdgcn_readlane(i1, 63)) return;      // (uniform)
+      // Sequences whose runs all come before this one.
+      seq = __popcll(__builtin_amdgcn_ballot_w64(i0 <= block)) +
+            __popcll(__builtin_amdgcn_ballot_w64(i1 <= block));
+      const int before = seq < 64 ? __builtin_amdgcn_readlane(i0 - r0, seq)
+                                  : __builtin_amdgcn_readlane(i1 - r1, seq - 64);
+      rt = tiles_of(seq);
+      parts = runs_of(rt.n, q);
+      row = (block - before) / parts;
+      part = (block - before) % parts;
+    }
+    first = run_begin(rt.n, parts, part);
+    last = run_begin(rt.n, parts, part + 1);
   } else {
     // Every thread adds up a run of sequences, a scan over the workgroup.
-    longest = 0;
+    const int each = (a.batch + NT - 1) / NT;
+    const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
+    int mine = 0, longest = 0;
     for (int b = b0; b < b1; ++b) {
       const int t = tiles_of(b).n;
       mine += t * rows;
       longest = max(longest, t);
     }
-    incl = mine;
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(incl, o, 64);
@@ -427,32 +487,30 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
       scan[1][wave] = longest;
     }
     __syncthreads();
-    total = 0;
+    int total = 0;
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       incl += w < wave ? scan[0][w] : 0;
       total += scan[0][w];
       longest = max(longest, scan[1][w]);
     }
     total = __builtin_amdgcn_readfirstlane(total);
     longest = __builtin_amdgcn_readfirstlane(longest);
-  }
-  if (rows_whole(longest, a.batch * rows, (int)gridDim.x)) {
-    if ((int)blockIdx.x >= a.batch * rows) return; // (uniform)
-    seq = (int)blockIdx.x / rows;
-    row = (int)blockIdx.x % rows;
-    rt = tiles_of(seq);
-    quota = longest;
-    begin = start = (int)blockIdx.x * quota;
-    end = begin + rt.n;
-  } else {
-    quota = quota_of(total, (int)gridDim.x);
-    begin = (int)blockIdx.x * quota;
-    if (begin >= total) return;                    // (uniform)
-    end = min(begin + quota, total);
-    int before = 0;
-    seq = 0;
-    if (a.batch > 1) {
+    if (rows_whole(longest, a.batch * rows, grid)) {
+      if (block >= a.batch * rows) return;         // (uniform)
+      seq = block / rows;
+      row = block % rows;
+      rt = tiles_of(seq);
+      quota = longest;
+      start = block * quota;
+      end = start + rt.n;
+      first = 0;
+      last = rt.n;
+    } else {
+      quota = quota_of(total, grid, W);
+      const int begin = block * quota;
+      if (begin >= total) return;                  // (uniform)
+      end = min(begin + quota, total);
       int at = incl - mine;
       if (begin >= at && begin < incl) {           // (one thread: runs without tiles are empty)
         int b = b0;
@@ -466,20 +524,24 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
       }
       __syncthreads();
       seq = __builtin_amdgcn_readfirstlane(found[0]);
-      before = __builtin_amdgcn_readfirstlane(found[1]);
+      const int before = __builtin_amdgcn_readfirstlane(found[1]);
+      rt = tiles_of(seq);
+      row = (begin - before) / rt.n;
+      start = before + row * rt.n;
+      first = begin - start;
+      last = min(end, start + rt.n) - start;
+      const RowShare share = row_share(start, rt.n, quota);
+      parts = share.last - share.first + 1;
+      part = block - share.first;
     }
-    rt = tiles_of(seq);
-    row = (begin - before) / rt.n;
-    start = before + row * rt.n;
   }
 
   for (;;) {
-    const int len = min(max(a.seq_len[seq], 0), a.len_max);
+    const int len = length(seq);
     const int lo = a.window > 0 ? max(0, len - a.window) : 0;
     const int kvh = row / a.hg, h0 = kvh * a.G + (row % a.hg) * kPagedHeads;
     const int heads = min(kPagedHeads, (kvh + 1) * a.G - h0);
     const int64_t q_row = (int64_t)seq * a.n_q_heads + h0;
-    const int first = max(begin, start) - start, last = min(end, start + rt.n) - start;
     const int32_t* table = a.table + seq * a.table_stride;
     const char* kb = a.k + kvh * a.head_stride;
     const char* vb = a.v + kvh * a.head_stride;
@@ -502,7 +564,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
 
     // Two tiles ahead: pages; one tile ahead: keys and values.
     int i = first + wave;
-    int t0 = rt.token(min(i, last - 1), TT), t1 = rt.token(min(i + kPagedWaves, last - 1), TT);
+    int t0 = rt.token(min(i, last - 1), TT), t1 = rt.token(min(i + W, last - 1), TT);
     int kp = page_of(t0, M::key_block(n)), vp = page_of(t0, M::value_block(g));
     int kp1 = page_of(t1, M::key_block(n)), vp1 = page_of(t1, M::value_block(g));
     typename M::template Query<QT> q;
@@ -520,12 +582,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
       key.load(key_row(t0, kp), a.tok_stride, g);
       val.load(value_row(t0, vp), a.tok_stride, n);
     }
-    for (; i < last; i += kPagedWaves) {
-      const bool more = i + kPagedWaves < last;
+    for (; i < last; i += W) {
+      const bool more = i + W < last;
       float z[NM];
       M::template scores<QT>(key, q, z);
       if (more) key.load(key_row(t1, kp1), a.tok_stride, g);
-      const int t2 = rt.token(min(i + 2 * kPagedWaves, last - 1), TT);
+      const int t2 = rt.token(min(i + 2 * W, last - 1), TT);
       const int kp2 = page_of(t2, M::key_block(n)), vp2 = page_of(t2, M::value_block(g));
       if (a.cap > 0.f) {
         const float in = a.scale / a.cap, out = a.cap * kLog2e;
@@ -589,8 +651,6 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
     }
     __syncthreads();
 
-    const RowShare share = row_share(start, rt.n, quota);
-    const int parts = share.last - share.first + 1;
     // What a row ends as: outputs and log-sum-exp, or a partial for another join.
     auto finish = [&](int h, int c4, float m, float l, v4f o) {
       if (a.seg) {
@@ -605,28 +665,28 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
     };
     // Part slots: Partial [kPagedHeads], stored and loaded where every compute unit sees them.
     const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, kPartsBytes, kRsrcWord3);
-    auto part_at = [&](int w, int h) {
-      return (part_slot(w, start, quota) * kPagedHeads + h) * (int)sizeof(Partial);
+    auto part_at = [&](int p, int h) {
+      const int w = block - part + p;
+      const int slot = RUNS ? w : part_slot(w, start, quota);
+      return (slot * kPagedHeads + h) * (int)sizeof(Partial);
     };
-    const int units = heads * (kD / 4);            // (head, four channels)
-    for (int x = tid; x < units; x += kPagedThreads) {
+    for (int x = tid; x < heads * (kD / 4); x += NT) {
       const int h = x / (kD / 4), c4 = x % (kD / 4);
       float m = sh.m[0][h];
 #pragma unroll
-      for (int w = 1; w < kPagedWaves; ++w) m = fmaxf(m, sh.m[w][h]);
+      for (int w = 1; w < W; ++w) m = fmaxf(m, sh.m[w][h]);
       float l = 0.f;
       v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kPagedWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = sh.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[w][h] - m);
         l += sh.l[w][h] == 0.f ? 0.f : f * sh.l[w][h];
-        const v4f s = *reinterpret_cast<const v4f*>(&sh.sums[w][h][4 * c4]);
-        o += f * s;
+        o += f * *reinterpret_cast<const v4f*>(&sh.sums[w][h][4 * c4]);
       }
       if (parts == 1) {
         finish(h, c4, m, l, o);
       } else {
-        const int off = part_at(blockIdx.x, h);
+        const int off = part_at(part, h);
         __builtin_amdgcn_raw_buffer_store_b128((v4i)o, slots, off + 16 + 16 * c4, 0, kCoherent);
         if (c4 == 0)
           __builtin_amdgcn_raw_buffer_store_b128((v4i)(v4f){m, l, 0.f, 0.f}, slots, off, 0,
@@ -641,21 +701,27 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
         arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (arrived == (unsigned)parts - 1u) {
-        join_parts(sh, parts, share.first, heads, finish, [&](int w, int h, int off) {
-          return (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, part_at(w, h) + off, 0,
+        join_parts(sh, parts, heads, finish, [&](int p, int h, int off) {
+          return (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, part_at(p, h) + off, 0,
                                                             kCoherent);
         });
         if (tid == 0) *counter = 0u;               // as the next call expects it
       }
     }
+    if constexpr (RUNS) return;
     start += rt.n;
-    if (start >= end) break;
+    if (start >= end) return;
     __syncthreads();                               // LDS is read: the next row's parts go there
     if (++row == rows) {
       row = 0;
       ++seq;
       rt = tiles_of(seq);
     }
+    first = 0;
+    last = min(end, start + rt.n) - start;
+    const RowShare share = row_share(start, rt.n, quota);
+    parts = share.last - share.first + 1;
+    part = block - share.first;
   }
 }
 
@@ -678,19 +744,28 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
   if (most > (1 << 30)) return AATC_E_UNSUPPORTED;
-  const int grid = (int)std::min<int64_t>(kPagedGroups, most);
+  const bool runs = rows <= kMaxRunRows;
+  const int grid = (int)std::min<int64_t>(runs ? kRunGroups : kLineGroups, most);
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kPagedThreads), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * (runs ? kRunWaves : kLineWaves)), 0,
+                       st, a);
     return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
   };
+  auto launch_as = [&](auto m, auto qt) {
+    using M = decltype(m);
+    constexpr int QT = decltype(qt)::value;
+    return runs ? launch(paged_kernel<M, QT, true>) : launch(paged_kernel<M, QT, false>);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Three = std::integral_constant<int, 3>;
   const bool same = a.q_dtype == (int)c_dtype;
   switch (c_dtype) {
-    case AATC_F32: return launch(paged_kernel<Full32, 1>);
+    case AATC_F32: return launch_as(Full32{}, One{});
     case AATC_BF16:
-      return same ? launch(paged_kernel<Half16<__bf16>, 1>) : launch(paged_kernel<Half16<__bf16>, 3>);
+      return same ? launch_as(Half16<__bf16>{}, One{}) : launch_as(Half16<__bf16>{}, Three{});
     default:
-      return same ? launch(paged_kernel<Half16<_Float16>, 1>) : launch(paged_kernel<Half16<_Float16>, 3>);
+      return same ? launch_as(Half16<_Float16>{}, One{}) : launch_as(Half16<_Float16>{}, Three{});
   }
 }
 

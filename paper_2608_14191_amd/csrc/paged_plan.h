@@ -34,21 +34,46 @@ AATC_PAGED_HD inline RowTiles row_tiles(int len, int window, int sink, int tt) {
   return r;
 }
 
-// Rows so short that one workgroup has each in a few rounds of its waves are not shared, if there
-// is a workgroup for every row.
+// Rows are shared out in one of two ways.
+//
+// Runs, for few rows: every row is cut into runs of nearly equal length, one workgroup each, none
+// longer than `rounds` tiles for each of its waves: the smallest such number with which the runs
+// of the batch fit the grid.  A workgroup then has one row only (to change rows in the middle
+// costs it the latencies of a new start, which few others cover).
+//
+// smallest_rounds: count(q) is the number of runs of at most q tiles, for all rows; `tiles` those
+// of all rows; rows < grid.
+constexpr int kRoundsMin = 2;         // (a join of parts takes longer than one round more)
+template <class Count>
+AATC_PAGED_HD inline int smallest_rounds(int tiles, int rows, int grid, int waves, Count count) {
+  int lo = (tiles + grid * waves - 1) / (grid * waves);          // the average: none lower fits
+  if (lo < kRoundsMin) lo = kRoundsMin;
+  if (count(lo * waves) <= grid) return lo;
+  // sum ceil(n / q) <= tiles / q + rows
+  int hi = (tiles + (grid - rows) * waves - 1) / ((grid - rows) * waves);
+  while (hi - lo > 1 + lo / 16) {                                // lo does not fit, hi does
+    const int mid = (lo + hi) / 2;
+    if (count(mid * waves) <= grid) hi = mid;
+    else lo = mid;
+  }
+  return hi;
+}
+AATC_PAGED_HD inline int runs_of(int n, int q) { return (n + q - 1) / q; }
+// Run i of `runs` has the row's tiles from here on.
+AATC_PAGED_HD inline int run_begin(int n, int runs, int i) { return (int)((int64_t)n * i / runs); }
+
+// Lines, for many rows: the tiles of all rows lie in one line, row after row; workgroup w takes
+// those from w quota on, of several rows or of a part of one.  Rows so short that one workgroup
+// has each in a few rounds of its waves are not cut if there is a workgroup for every row.
 constexpr int kWholeRow = 32;
 AATC_PAGED_HD inline bool rows_whole(int longest, int rows, int grid) {
   return longest <= kWholeRow && rows <= grid;
 }
-
 // Else: tiles of a workgroup, one for each of its waves at least.
-constexpr int kQuotaMin = 8;
-AATC_PAGED_HD inline int quota_of(int total, int grid) {
-  const int even = (total + grid - 1) / grid;
-  return even > kQuotaMin ? even : kQuotaMin;
+AATC_PAGED_HD inline int quota_of(int tiles, int grid, int waves) {
+  const int even = (tiles + grid - 1) / grid;
+  return even > waves ? even : waves;
 }
-
-// The tiles of all rows lie in one line, row after row; workgroup w takes those from w quota on.
 // A row that starts at `start` with n tiles is shared by the workgroups first .. last.
 struct RowShare {
   int first, last;

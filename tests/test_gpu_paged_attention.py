@@ -129,6 +129,15 @@ def test_splits(lens, cache):
     _check(_case(8, lens, 4, 2, 16, cache))
 
 
+@pytest.mark.parametrize("hq,hkv,lens", [
+    (16, 1, [9000]), (40, 2, [6000, 3, 4100]), (1, 1, [20000]),           # runs, many heads to join
+    (1, 1, [40 * i for i in range(128)]), (2, 1, [7] * 65 + [6000] + [0] * 62),   # 128 rows
+    (64, 4, [5] * 33 + [8000]), (16, 1, [0] * 150 + [5000, 9000]),        # lines, a row in many
+    (7, 1, [600] * 129), (4, 4, [1100, 20] * 30)])
+def test_splits_of_rows(hq, hkv, lens):
+    _check(_case(12, lens, hq, hkv, 64))
+
+
 def test_peaked_scores_and_far_maximum():
     """Queries along one key (a weight near 1), and scores far below the maximum."""
     k, v, table, lens, q = _case(9, [900, 1200], 4, 2, 16, "f16", "f32")
