@@ -9,6 +9,7 @@ call reads or writes.  Entry points are bound at their first use.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import numpy as np
 
@@ -35,6 +36,7 @@ class Rope(ctypes.Structure):
         _on_device("Rope", freq)
         super().__init__(freq.data_ptr(), 2 * freq.numel(), int(layout), float(factor))
         self.tensor = freq
+        self.address = ctypes.addressof(self)
 
 
 class PagedCache(ctypes.Structure):
@@ -57,67 +59,100 @@ class PagedCache(ctypes.Structure):
         super().__init__(k_pages.data_ptr(), v_pages.data_ptr(), _dtype(k_pages), heads, d, tokens,
                          n_pages, page, head, tok)
         self.tensors = (k_pages, v_pages)
+        self.address = ctypes.addressof(self)
 
 
 class PageTable(ctypes.Structure):
-    """aatc_page_table of an int32 tensor [rows][max_pages] (rows may be padded)."""
+    """aatc_page_table of an int32 tensor [rows][max_pages] (rows may be padded), kept alive here.
+    The calls below also take the tensor itself."""
 
     _fields_ = [("table", _vp), ("stride", _i64), ("rows", _i32), ("max_pages", _i32)]
 
     def __init__(self, table):
-        rows, entries = table.shape
-        if table.dtype != _torch().int32 or (entries > 1 and table.stride(1) != 1):
-            raise TypeError("a page table must be an int32 tensor [rows][max_pages], rows contiguous")
-        _on_device("PageTable", table)
-        super().__init__(table.data_ptr(), table.stride(0) if rows > 1 else entries, rows, entries)
+        packed, _ = _table("PageTable", table, _on_device("PageTable", table))
+        super().__init__(*struct.unpack("=Qqii", packed))
+        self.tensor = table
 
 
+# Marshalling: the shortest kernels take 3 us, so the checks are plain attribute reads, error
+# texts are made only when an error is raised, and a page table given as a tensor goes as 24
+# packed bytes.
 _TORCH = None
 _DTYPES = {}
+_device = _raw_stream = None
+_pack_table = struct.Struct("=Qqii").pack
 
 
 def _torch():
-    global _TORCH
+    global _TORCH, _device, _raw_stream
     if _TORCH is None:
         import torch
-        _TORCH = torch
         _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _TORCH = torch
     return _TORCH
 
 
 def _dtype(t) -> int:
-    _torch()
     code = _DTYPES.get(t.dtype)
     if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype}")
+        _torch()
+        code = _DTYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {t.dtype}")
     return code
 
 
-def _on_device(func: str, *tensors):
-    """Tensors (None allowed) must be on the current device: kernels are launched there."""
-    device = _torch().cuda.current_device()
+def _on_device(func: str, *tensors) -> int:
+    """Tensors (None allowed) must be on the current device, where kernels are launched: its
+    index."""
+    if not _torch().cuda.is_initialized():
+        _TORCH.cuda.init()
+    device = _device()
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise AatcError(f"{func} (a tensor is on {t.device}, the current device is cuda:{device})",
-                            E_INVALID)
+            _refuse(func, f"a tensor is on {t.device}, the current device is cuda:{device}")
+    return device
 
 
-def _want(func: str, what: str, ok: bool):
-    if not ok:
-        raise AatcError(f"{func} ({what})", E_INVALID)
+def _refuse(func: str, why: str):
+    raise AatcError(f"{func} ({why})", E_INVALID)
 
 
 def _list(func: str, name: str, t, n: int):
     """An int32 tensor that n numbers are read from or written to."""
-    _want(func, f"{name} must be a contiguous int32 tensor of at least {n}",
-          t.dtype == _TORCH.int32 and t.is_contiguous() and t.numel() >= n)
+    if t.dtype != _TORCH.int32 or not t.is_contiguous() or t.numel() < n:
+        _refuse(func, f"{name} must be a contiguous int32 tensor of at least {n}")
+
+
+def _floats(func: str, name: str, t, n: int):
+    if t.dtype != _TORCH.float32 or not t.is_contiguous() or t.numel() < n:
+        _refuse(func, f"{name} must be a contiguous float32 tensor of at least {n}")
 
 
 def _tokens(func: str, name: str, t, n_tok: int, stride: int, heads: int):
     """A view whose first element is token 0's: the storage must reach the last token's end."""
-    need = (n_tok - 1) * stride + heads * HEAD_DIM if n_tok > 0 else 0
+    need = (n_tok - 1) * stride + heads * HEAD_DIM
+    if n_tok <= 0 or (t.is_contiguous() and t.numel() >= need):
+        return
     have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-    _want(func, f"{name} holds {have} elements from its first on, {need} are used", have >= need)
+    if have < need:
+        _refuse(func, f"{name} holds {have} elements from its first on, {need} are used")
+
+
+def _table(func: str, table, device: int):
+    """(aatc_page_table as an argument, rows) of a PageTable or an int32 tensor."""
+    if isinstance(table, PageTable):
+        return ctypes.addressof(table), table.rows
+    rows, entries = table.shape
+    across, along = table.stride()
+    if table.dtype != _TORCH.int32 or (entries > 1 and along != 1):
+        _refuse(func, "a page table must be an int32 tensor [rows][max_pages], rows contiguous")
+    if table.get_device() != device:
+        _refuse(func, f"the page table is on {table.device}, the current device is cuda:{device}")
+    return _pack_table(table.data_ptr(), across if rows > 1 else entries, rows, entries), rows
 
 
 _SIGNATURES = {
@@ -176,14 +211,17 @@ def aatc_rope(x, n_tok: int, n_heads: int, x_tok_stride: int, pos, rope: Rope, o
               out_tok_stride: int, inverse: bool = False, stream=None):
     """Rotates n_tok tokens of x ([n_heads][128] at every x_tok_stride elements) into out."""
     f = "aatc_rope"
-    _on_device(f, x, pos, out, rope.tensor)
-    _want(f, "x and out differ in type", x.dtype == out.dtype)
+    device = _on_device(f, x, pos, out, rope.tensor)
+    if x.dtype != out.dtype:
+        _refuse(f, "x and out differ in type")
     _list(f, "pos", pos, n_tok)
     _tokens(f, "x", x, n_tok, x_tok_stride, n_heads)
     _tokens(f, "out", out, n_tok, out_tok_stride, n_heads)
-    _check(f, entry_point(f)(_ptr(x), _dtype(x), n_tok, n_heads, HEAD_DIM, x_tok_stride, _ptr(pos),
-                             ctypes.addressof(rope), 1 if inverse else 0, _ptr(out),
-                             out_tok_stride, _lib._stream(stream)))
+    status = entry_point(f)(x.data_ptr(), _dtype(x), n_tok, n_heads, HEAD_DIM, x_tok_stride,
+                            pos.data_ptr(), rope.address, 1 if inverse else 0, out.data_ptr(),
+                            out_tok_stride, _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_paged_append(cache: PagedCache, table, n_tok: int, k, v, k_tok_stride: int,
@@ -191,22 +229,30 @@ def aatc_paged_append(cache: PagedCache, table, n_tok: int, k, v, k_tok_stride: 
                       q_tok_stride: int = 0, q_out=None, q_out_tok_stride: int = 0, stream=None):
     """Stores n_tok new tokens in the pages of their sequences, keys (and q, into q_out) rotated."""
     f = "aatc_paged_append"
-    _on_device(f, k, v, seq, pos, q, q_out, cache.tensors[0], rope.tensor if rope else None)
-    _want(f, "q, k and v differ in type", k.dtype == v.dtype and
-          (q is None or (q.dtype == k.dtype and q_out is not None and q_out.dtype == k.dtype)))
+    device = _on_device(f, k, v, seq, pos, q, q_out, cache.tensors[0],
+                        None if rope is None else rope.tensor)
+    x = k.dtype
+    if v.dtype != x:
+        _refuse(f, "q, k and v differ in type")
+    heads = cache.n_kv_heads
     _list(f, "pos", pos, n_tok)
     if seq is not None:
         _list(f, "seq", seq, n_tok)
-    _tokens(f, "k", k, n_tok, k_tok_stride, cache.n_kv_heads)
-    _tokens(f, "v", v, n_tok, v_tok_stride, cache.n_kv_heads)
+    _tokens(f, "k", k, n_tok, k_tok_stride, heads)
+    _tokens(f, "v", v, n_tok, v_tok_stride, heads)
     if q is not None:
+        if q_out is None or q.dtype != x or q_out.dtype != x:
+            _refuse(f, "q, q_out and k differ in type")
         _tokens(f, "q", q, n_tok, q_tok_stride, n_q_heads)
         _tokens(f, "q_out", q_out, n_tok, q_out_tok_stride, n_q_heads)
-    t = PageTable(table)
-    _check(f, entry_point(f)(ctypes.addressof(cache), ctypes.addressof(t), n_tok, _dtype(k),
-                             _ptr(k), k_tok_stride, _ptr(v), v_tok_stride, _ptr(seq), _ptr(pos),
-                             ctypes.addressof(rope) if rope else None, n_q_heads, _ptr(q),
-                             q_tok_stride, _ptr(q_out), q_out_tok_stride, _lib._stream(stream)))
+    t, _ = _table(f, table, device)
+    status = entry_point(f)(cache.address, t, n_tok, _dtype(k), k.data_ptr(), k_tok_stride,
+                            v.data_ptr(), v_tok_stride, _ptr(seq), pos.data_ptr(),
+                            None if rope is None else rope.address, n_q_heads, _ptr(q),
+                            q_tok_stride, _ptr(q_out), q_out_tok_stride,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_paged_decode_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: int) -> int:
@@ -224,22 +270,22 @@ def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n
     """Attention of one token per sequence (q: [batch][n_q_heads][128], rows q_stride elements
     apart) over the pages; out [batch][n_q_heads][128] and lse [batch][n_q_heads] in float32."""
     f = "aatc_paged_decode_attention"
-    _on_device(f, seq_len, q, out, workspace, slopes, lse, cache.tensors[0])
-    fp32 = _TORCH.float32
+    device = _on_device(f, seq_len, q, out, workspace, slopes, lse, cache.tensors[0])
     _list(f, "seq_len", seq_len, batch)
-    _want(f, "out must be a contiguous float32 tensor [batch][n_q_heads][128]",
-          out.dtype == fp32 and out.is_contiguous() and out.numel() >= batch * n_q_heads * HEAD_DIM)
-    for name, t, n in (("lse", lse, batch * n_q_heads), ("slopes", slopes, n_q_heads)):
-        if t is not None:
-            _want(f, f"{name} must be a contiguous float32 tensor of at least {n}",
-                  t.dtype == fp32 and t.is_contiguous() and t.numel() >= n)
+    _floats(f, "out", out, batch * n_q_heads * HEAD_DIM)
+    if lse is not None:
+        _floats(f, "lse", lse, batch * n_q_heads)
+    if slopes is not None:
+        _floats(f, "slopes", slopes, n_q_heads)
     stride = n_q_heads * HEAD_DIM if q_stride is None else q_stride
     _tokens(f, "q", q, batch, stride, n_q_heads)
-    t = PageTable(table)
-    _check(f, entry_point(f)(ctypes.addressof(cache), ctypes.addressof(t), _ptr(seq_len), batch,
-                             n_q_heads, _ptr(q), _dtype(q), stride, softmax_scale, window, sink,
-                             softcap, _ptr(slopes), _ptr(out), _ptr(lse), _ptr(workspace),
-                             _bytes(workspace), _lib._stream(stream)))
+    t, _ = _table(f, table, device)
+    status = entry_point(f)(cache.address, t, seq_len.data_ptr(), batch, n_q_heads, q.data_ptr(),
+                            _dtype(q), stride, softmax_scale, window, sink, softcap, _ptr(slopes),
+                            out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_decode_paged_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: int,
@@ -254,51 +300,56 @@ def aatc_decode_attention_paged(dev_params_k, dev_params_v, batch: int, n_q_head
                                 workspace, stream=None):
     """Decode attention over the compressed caches plus the page_len tokens of the pages."""
     f = "aatc_decode_attention_paged"
-    _on_device(f, dev_params_k, dev_params_v, q, k_codes, k_alpha, v_codes, v_alpha, seq_len,
-               page_len, out, workspace, cache.tensors[0])
+    device = _on_device(f, dev_params_k, dev_params_v, q, k_codes, k_alpha, v_codes, v_alpha,
+                        seq_len, page_len, out, workspace, cache.tensors[0])
     _list(f, "seq_len", seq_len, batch)
     _list(f, "page_len", page_len, batch)
-    _want(f, "out must be a contiguous float32 tensor [batch][n_q_heads][128]",
-          out.dtype == _TORCH.float32 and out.is_contiguous() and
-          out.numel() >= batch * n_q_heads * HEAD_DIM)
+    _floats(f, "out", out, batch * n_q_heads * HEAD_DIM)
     _tokens(f, "q", q, batch, n_q_heads * HEAD_DIM, n_q_heads)
-    t = PageTable(table)
-    _check(f, entry_point(f)(
-        _ptr(dev_params_k), _ptr(dev_params_v), batch, n_q_heads, n_kv_heads, HEAD_DIM, _ptr(q),
-        _dtype(q), _ptr(k_codes), _ptr(k_alpha), _ptr(v_codes), _ptr(v_alpha), _ptr(seq_len), cap,
-        k_record_bytes, v_record_bytes, softmax_scale, ctypes.addressof(cache),
-        ctypes.addressof(t), _ptr(page_len), _ptr(out), _ptr(workspace), _bytes(workspace),
-        _lib._stream(stream)))
+    t, _ = _table(f, table, device)
+    status = entry_point(f)(
+        dev_params_k.data_ptr(), dev_params_v.data_ptr(), batch, n_q_heads, n_kv_heads, HEAD_DIM,
+        q.data_ptr(), _dtype(q), k_codes.data_ptr(), k_alpha.data_ptr(), v_codes.data_ptr(),
+        v_alpha.data_ptr(), seq_len.data_ptr(), cap, k_record_bytes, v_record_bytes, softmax_scale,
+        cache.address, t, page_len.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+        workspace.nbytes, _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
-# Page tables: `table` int32 [rows][max_pages], `ref` int32 [n_pages] (include/aatc_paged.h).
-def _pairs(func: str, name: str, t, n: int):
-    _want(func, f"{name} must be a contiguous int32 tensor [{n}][2]",
-          t.dtype == _TORCH.int32 and t.is_contiguous() and t.numel() >= 2 * n)
-
-
+# Page tables: `table` int32 [rows][max_pages] (or a PageTable), `ref` int32 [n_pages]
+# (include/aatc_paged.h).
 def aatc_pages_fork(src_table, dst_table, ref, pairs, stream=None):
     """dst_table's rows pairs[:, 1] become copies of src_table's rows pairs[:, 0]."""
     f = "aatc_pages_fork"
-    _on_device(f, ref, pairs)
-    n = pairs.shape[0]
-    _pairs(f, "pairs", pairs, n)
+    device = _on_device(f, ref, pairs)
+    n = len(pairs)
+    _list(f, "pairs", pairs, 2 * n)
     _list(f, "ref", ref, 1)
-    src, dst = PageTable(src_table), PageTable(dst_table)
-    _check(f, entry_point(f)(ctypes.addressof(src), ctypes.addressof(dst), _ptr(ref), ref.numel(),
-                             _ptr(pairs) or None, n, _lib._stream(stream)) if n else 0)
+    src, _ = _table(f, src_table, device)
+    dst, _ = _table(f, dst_table, device)
+    if n == 0:
+        return
+    status = entry_point(f)(src, dst, ref.data_ptr(), ref.numel(), pairs.data_ptr(), n,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_pages_free(table, ref, rows, stream=None):
     """Empties the rows listed (int32 tensor)."""
     f = "aatc_pages_free"
-    _on_device(f, ref, rows)
+    device = _on_device(f, ref, rows)
     n = rows.numel()
     _list(f, "rows", rows, n)
     _list(f, "ref", ref, 1)
-    t = PageTable(table)
-    _check(f, entry_point(f)(ctypes.addressof(t), _ptr(ref), ref.numel(), _ptr(rows), n,
-                             _lib._stream(stream)) if n else 0)
+    t, _ = _table(f, table, device)
+    if n == 0:
+        return
+    status = entry_point(f)(t, ref.data_ptr(), ref.numel(), rows.data_ptr(), n,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_pages_workspace_bytes(rows: int, n_pages: int) -> int:
@@ -310,48 +361,59 @@ def aatc_pages_reserve(table, ref, page_tokens: int, held, wanted, pairs, lackin
     """Pages for the tokens held[b] .. wanted[b] - 1 of every row; pairs [rows][2] to copy,
     lacking [1]."""
     f = "aatc_pages_reserve"
-    _on_device(f, ref, held, wanted, pairs, lacking, workspace)
-    rows = table.shape[0]
-    for name, t in (("held", held), ("wanted", wanted)):
-        _list(f, name, t, rows)
+    device = _on_device(f, ref, held, wanted, pairs, lacking, workspace)
+    t, rows = _table(f, table, device)
+    _list(f, "held", held, rows)
+    _list(f, "wanted", wanted, rows)
     _list(f, "ref", ref, 1)
     _list(f, "lacking", lacking, 1)
-    _pairs(f, "pairs", pairs, rows)
-    t = PageTable(table)
-    _check(f, entry_point(f)(ctypes.addressof(t), _ptr(ref), ref.numel(), page_tokens, _ptr(held),
-                             _ptr(wanted), _ptr(pairs), _ptr(lacking), _ptr(workspace),
-                             _bytes(workspace), _lib._stream(stream)))
+    _list(f, "pairs", pairs, 2 * rows)
+    status = entry_point(f)(t, ref.data_ptr(), ref.numel(), page_tokens, held.data_ptr(),
+                            wanted.data_ptr(), pairs.data_ptr(), lacking.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_pages_compact(table, ref, table_out, ref_out, pairs, moves, workspace, stream=None):
     """The table and counts with the pages in use moved to the front, and the moves
     (pairs [n_pages / 2][2], moves [1]) for aatc_pages_copy."""
     f = "aatc_pages_compact"
-    _on_device(f, ref, ref_out, pairs, moves, workspace)
+    device = _on_device(f, ref, ref_out, pairs, moves, workspace)
     n_pages = ref.numel()
     _list(f, "ref", ref, 1)
     _list(f, "ref_out", ref_out, n_pages)
     _list(f, "moves", moves, 1)
-    _pairs(f, "pairs", pairs, n_pages // 2)
-    t, o = PageTable(table), PageTable(table_out)
-    _check(f, entry_point(f)(ctypes.addressof(t), _ptr(ref), n_pages, ctypes.addressof(o),
-                             _ptr(ref_out), _ptr(pairs), _ptr(moves), _ptr(workspace),
-                             _bytes(workspace), _lib._stream(stream)))
+    _list(f, "pairs", pairs, n_pages // 2 * 2)
+    t, _ = _table(f, table, device)
+    o, _ = _table(f, table_out, device)
+    status = entry_point(f)(t, ref.data_ptr(), n_pages, o, ref_out.data_ptr(), pairs.data_ptr(),
+                            moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
 
 
 def aatc_pages_copy(pools, pairs, n_pairs=None, stream=None):
     """Copies page pairs[i][0] to pairs[i][1] in every pool of `pools` ([pool][page][...], pages
     contiguous); n_pairs: int32 tensor [1], copy no more pairs than that."""
     f = "aatc_pages_copy"
-    _on_device(f, pools, pairs, n_pairs)
-    n = pairs.shape[0]
-    _pairs(f, "pairs", pairs, n)
+    device = _on_device(f, pools, pairs, n_pairs)
+    n = len(pairs)
+    _list(f, "pairs", pairs, 2 * n)
     if n_pairs is not None:
         _list(f, "n_pairs", n_pairs, 1)
-    _want(f, "pools must be [pool][page][...] with contiguous pages, one behind the other",
-          pools.dim() >= 3 and pools[0].is_contiguous())
-    page_bytes = pools[0, 0].numel() * pools.element_size()
+    if pools.dim() < 3 or not (pools.is_contiguous() or pools[0].is_contiguous()):
+        _refuse(f, "pools must be [pool][page][...] with contiguous pages, one behind the other")
     n_pools, n_pages = pools.shape[:2]
-    stride = pools.stride(0) * pools.element_size() if n_pools > 1 else n_pages * page_bytes
-    _check(f, entry_point(f)(_ptr(pools), n_pools, stride, n_pages, page_bytes, _ptr(pairs), n,
-                             _ptr(n_pairs), _lib._stream(stream)) if n else 0)
+    if n == 0 or pools.numel() == 0:
+        return
+    size = pools.element_size()
+    page_bytes = pools.numel() // (n_pools * n_pages) * size
+    stride = pools.stride(0) * size if n_pools > 1 else n_pages * page_bytes
+    status = entry_point(f)(pools.data_ptr(), n_pools, stride, n_pages, page_bytes,
+                            pairs.data_ptr(), n, _ptr(n_pairs),
+                            _raw_stream(device) if stream is None else int(stream))
+    if status:
+        raise AatcError(f, status)
