@@ -160,8 +160,8 @@ aatc_status aatc_paged_append(const aatc_paged_cache* cache, const aatc_page_tab
  * out       device [batch][n_q_heads][d] fp32, 16-byte aligned.
  * lse       device [batch][n_q_heads] fp32 or NULL.
  * workspace device scratch of aatc_paged_decode_workspace_bytes bytes, 256-byte aligned,
- *           zero-filled once after allocation; every call leaves it reusable.  Calls that may
- *           overlap need one each.
+ *           zero-filled once after allocation; every call leaves it reusable, for calls of other
+ *           shapes that it is large enough for too.  Calls that may overlap need one each.
  * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; more than 2^30 tiles of 16 tokens),
  * AATC_E_WORKSPACE, AATC_E_DEVICE.
  */
@@ -185,7 +185,8 @@ aatc_status aatc_paged_decode_attention(const aatc_paged_cache* cache,
  * q             device [batch][n_q_heads][d] contiguous, F32 or BF16, as aatc_decode_attention.
  * cache         n_kv_heads as the compressed cache's.
  * page_len      device [batch] int32, clamped to [0, max_pages * page_tokens].
- * workspace     of aatc_decode_paged_workspace_bytes bytes, 256-byte aligned, zero-filled once.
+ * workspace     of aatc_decode_paged_workspace_bytes bytes, 256-byte aligned, zero-filled once, and
+ *               again before calls of another batch, other head counts or another cap.
  * Other arguments and errors as in aatc_decode_attention.
  */
 size_t aatc_decode_paged_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,

@@ -41,7 +41,9 @@ constexpr int kLineWaves = 4, kLineGroups = 512;
 constexpr int kMaxRunRows = 128;                  // two sequences a lane (every row counts one)
 constexpr int kPagedHeads = 16;                   // query heads of a row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kPartsBytes = 2 * kLineGroups * kPagedHeads * (int)sizeof(Partial);
+// The workspace: part slots, two a wave of the lines, then the counters.  (The slots' size is fixed
+// so that the counters, which every call leaves at zero, are in one place for calls of any shape.)
+constexpr int kPartsBytes = 2 * kLineGroups * kLineWaves * kPagedHeads * (int)sizeof(Partial);
 constexpr int kRowStride = 64;                    // counters 256 bytes apart (their atomics
                                                   // would queue on one cache line)
 constexpr int kRsrcWord3 = 0x00020000;            // raw buffer descriptor word 3 (gfx950)
@@ -401,17 +403,283 @@ __device__ inline void join_parts(JoinSpace<W, GROUPS>& sh, int parts, int heads
   }
 }
 
+// What a row ends as: outputs and log-sum-exp, or a partial for another join.  Four channels of a
+// head.
+__device__ inline void finish_row(const PagedArgs& a, int64_t head, int c4, float m, float l, v4f o) {
+  if (a.seg) {
+    Partial* s = a.seg + head;
+    reinterpret_cast<v4f*>(s->o)[c4] = o;
+    if (c4 == 0) *reinterpret_cast<v4f*>(s) = (v4f){m, l, 0.f, 0.f};
+    return;
+  }
+  const v4f zero = {0.f, 0.f, 0.f, 0.f};
+  reinterpret_cast<v4f*>(a.out)[head * (kD / 4) + c4] = l == 0.f ? zero : o / l;
+  if (a.lse && c4 == 0) a.lse[head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// What one wave has of a row: for head n of its lanes the maximum, the sum and the value sums
+// (acc[j][r]: channel M::channel(j, r, g)) over the tiles first, first + step .. below last.
+struct RowPart {
+  float m, l;
+  v4f acc[8];
+};
+
+// A row: query heads h0 .. h0 + heads - 1 of sequence `seq` on KV head `kvh`.
+struct Row {
+  int len, kvh, h0, heads;
+  int64_t q_row;
+};
+__device__ inline Row row_of(const PagedArgs& a, int seq, int row) {
+  Row r;
+  r.len = min(max(a.seq_len[seq], 0), a.len_max);
+  r.kvh = row / a.hg;
+  r.h0 = r.kvh * a.G + (row % a.hg) * kPagedHeads;
+  r.heads = min(kPagedHeads, (r.kvh + 1) * a.G - r.h0);
+  r.q_row = (int64_t)seq * a.n_q_heads + r.h0;
+  return r;
+}
+
+template <class M, int QT>
+__device__ __forceinline__ void attend(const PagedArgs& a, int seq, const Row& r,
+                                       const RowTiles& rt, int first, int last, int step,
+                                       RowPart& out) {
+  constexpr int TT = M::kTokens, NM = M::kMine;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int lo = a.window > 0 ? max(0, r.len - a.window) : 0;
+  const int32_t* table = a.table + seq * a.table_stride;
+  const char* kb = a.k + r.kvh * a.head_stride;
+  const char* vb = a.v + r.kvh * a.head_stride;
+
+  // Page of the 8-token block `blk` of the tile at token t0 (-1: none there).
+  auto page_of = [&](int t0, int blk) {
+    const int i = (t0 + 8 * blk) >> a.page_shift;
+    return i < a.max_pages ? table[i] : -1;
+  };
+  auto exists = [&](int page) { return (page >= 0) & (page < a.n_pages); };
+  const int slot_mask = (1 << a.page_shift) - 1;
+  auto key_row = [&](int t0, int page) {
+    const int t = t0 + M::key_token(0, n);
+    return kb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
+  };
+  auto value_row = [&](int t0, int page) {
+    const int t = t0 + NM * g;
+    return vb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
+  };
+
+  // Two tiles ahead: pages; one tile ahead: keys and values.
+  int i = first;
+  int t0 = rt.token(min(i, last - 1), TT), t1 = rt.token(min(i + step, last - 1), TT);
+  int kp = page_of(t0, M::key_block(n)), vp = page_of(t0, M::value_block(g));
+  int kp1 = page_of(t1, M::key_block(n)), vp1 = page_of(t1, M::value_block(g));
+  typename M::template Query<QT> q;
+  q.load(a.q, a.q_dtype, (int64_t)seq * a.q_stride + (int64_t)(r.h0 + min(n, r.heads - 1)) * kD,
+         n < r.heads, g);
+  const float slope = a.slopes && n < r.heads ? a.slopes[r.h0 + n] * kLog2e : 0.f;
+
+  float m_run = -INFINITY, l_run = 0.f;
+  v4f(&acc)[8] = out.acc;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
+  typename M::Keys key;
+  typename M::Values val;
+  if (i < last) {
+    key.load(key_row(t0, kp), a.tok_stride, g);
+    val.load(value_row(t0, vp), a.tok_stride, n);
+  }
+  for (; i < last; i += step) {
+    const bool more = i + step < last;
+    float z[NM];
+    M::template scores<QT>(key, q, z);
+    if (more) key.load(key_row(t1, kp1), a.tok_stride, g);
+    const int t2 = rt.token(min(i + 2 * step, last - 1), TT);
+    const int kp2 = page_of(t2, M::key_block(n)), vp2 = page_of(t2, M::value_block(g));
+    if (a.cap > 0.f) {
+      const float in = a.scale / a.cap, out = a.cap * kLog2e;
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] = out * tanh_of(z[e] * in);
+    } else {
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] *= a.scale * kLog2e;
+    }
+    if (a.slopes) {
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] -= slope * (float)(r.len - 1 - (t0 + NM * g + e));
+    }
+    // A tile that is attended as a whole needs no masks.
+    const bool there = exists(vp);
+    const bool whole = t0 + TT <= r.len && (t0 >= lo || t0 + TT <= a.sink) &&
+                       __builtin_amdgcn_ballot_w64(!there) == 0;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < NM; ++e) {
+        const int t = t0 + NM * g + e;
+        // (no short circuits: selects, not branches)
+        const bool on = there & (t < r.len) & ((t >= lo) | (t < a.sink));
+        z[e] = on ? z[e] : -INFINITY;
+        val.keep(e, on);
+      }
+    }
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < NM; ++e) m = fmaxf(m, z[e]);
+    m = fmaxf(m_run, over_groups_max(m) - M::kLower);
+    const float ref = m == -INFINITY ? 0.f : m;
+    const float sa = __builtin_amdgcn_exp2f(m_run - ref);      // (0 at the first tile)
+    float p[NM], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < NM; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
+      sum += p[e];
+    }
+    l_run = l_run * sa + sum;
+    m_run = m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] *= sa;
+    M::accumulate(val, p, acc);
+    if (more) val.load(value_row(t1, vp1), a.tok_stride, n);
+    t0 = t1, vp = vp1;
+    t1 = t2, kp1 = kp2, vp1 = vp2;
+  }
+  out.m = m_run;
+  out.l = over_groups_sum(l_run);
+}
+
+// Lines of waves: every wave takes its tiles, or its row, for itself.  Rows that a wave has whole
+// need no join; the others are joined by the last of their waves.  `before`, `mine`: tiles before
+// and of this thread's sequences b0 ...
+template <class M, int QT>
+__device__ __forceinline__ void line_of_waves(const PagedArgs& a, LineWay way, int total,
+                                              int before, int mine, int b0, int (*found)[2],
+                                              __amdgpu_buffer_rsrc_t slots) {
+  constexpr int W = kLineWaves;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int me = (int)blockIdx.x * W + wave;
+  const int rows = a.n_kv_heads * a.hg, quota = way.quota;
+  auto tiles_of = [&](int b) {
+    return row_tiles(min(max(a.seq_len[b], 0), a.len_max), a.window, a.sink, M::kTokens);
+  };
+  int seq, row, start, end;
+  RowTiles rt;
+  if (way.whole) {
+    if (me >= a.batch * rows) return;
+    seq = me / rows;
+    row = me % rows;
+    rt = tiles_of(seq);
+    start = me * quota;
+    end = start + rt.n;
+  } else {
+    for (int w = 0; w < W; ++w) {                  // (one thread finds each: no other has the tile)
+      const int x = ((int)blockIdx.x * W + w) * quota;
+      if (x >= before && x < before + mine) {
+        int b = b0, at = before;
+        for (;; ++b) {
+          const int t = tiles_of(b).n * rows;
+          if (x < at + t) break;
+          at += t;
+        }
+        found[w][0] = b;
+        found[w][1] = at;
+      }
+    }
+    __syncthreads();
+    const int begin = me * quota;
+    if (begin >= total) return;
+    end = min(begin + quota, total);
+    seq = __builtin_amdgcn_readfirstlane(found[wave][0]);
+    const int at = __builtin_amdgcn_readfirstlane(found[wave][1]);
+    rt = tiles_of(seq);
+    row = (begin - at) / rt.n;
+    start = at + row * rt.n;
+  }
+  for (;;) {
+    const Row r = row_of(a, seq, row);
+    const RowShare share = row_share(start, rt.n, quota);
+    const int parts = share.last - share.first + 1;
+    const int first = max(me * quota - start, 0), last = min(end - start, rt.n);
+    RowPart x;
+    attend<M, QT>(a, seq, r, rt, first, last, 1, x);
+    auto part_at = [&](int p, int h) {
+      return (part_slot(share.first + p, start, quota) * a.slot_heads + h) * (int)sizeof(Partial);
+    };
+    if (n < r.heads) {
+#pragma unroll
+      for (int j = 0; j < 8; j += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = M::channel(j, i, g);
+          const v4f o = {x.acc[j][i], x.acc[j + 1][i], x.acc[j + 2][i], x.acc[j + 3][i]};
+          if (parts == 1)
+            finish_row(a, r.q_row + n, c / 4, x.m, x.l, o);
+          else
+            __builtin_amdgcn_raw_buffer_store_b128((v4i)o, slots,
+                                                   part_at(me - share.first, n) + 16 + 4 * c, 0,
+                                                   kCoherent);
+        }
+      if (parts > 1 && g == 0)
+        __builtin_amdgcn_raw_buffer_store_b128((v4i)(v4f){x.m, x.l, 0.f, 0.f}, slots,
+                                               part_at(me - share.first, n), 0, kCoherent);
+    }
+    if (parts > 1) {
+      unsigned* counter = a.counters + ((int64_t)seq * rows + row) * kRowStride;
+      __builtin_amdgcn_s_waitcnt(0);               // the wave's stores are done
+      unsigned before_me = 0u;
+      if (lane == 0)
+        before_me = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (__builtin_amdgcn_readfirstlane(before_me) == (unsigned)parts - 1u) {
+        constexpr int U = 4;                       // parts in flight
+        for (int u = lane; u < r.heads * (kD / 4); u += 64) {
+          const int h = u / (kD / 4), c4 = u % (kD / 4);
+          float m = -INFINITY, l = 0.f;
+          v4f o = {0.f, 0.f, 0.f, 0.f};
+          for (int p0 = 0; p0 < parts; p0 += U) {
+            v4f ml[U], po[U];
+#pragma unroll
+            for (int p = 0; p < U; ++p) {
+              const int at = part_at(min(p0 + p, parts - 1), h);
+              ml[p] = (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, at, 0, kCoherent);
+              po[p] = (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, at + 16 + 16 * c4, 0, kCoherent);
+            }
+#pragma unroll
+            for (int p = 0; p < U; ++p) {
+              const bool on = (p0 + p < parts) & (ml[p][1] != 0.f);    // (NaN counts)
+              const float top = on ? fmaxf(m, ml[p][0]) : m;
+              const float ref = top == -INFINITY ? 0.f : top;
+              const float fa = __builtin_amdgcn_exp2f(m - ref);
+              const float fb = on ? __builtin_amdgcn_exp2f(ml[p][0] - ref) : 0.f;
+              l = l * fa + (on ? ml[p][1] * fb : 0.f);
+              o = o * fa + fb * po[p];
+              m = top;
+            }
+          }
+          finish_row(a, r.q_row + h, c4, m, l, o);
+        }
+        if (lane == 0) *counter = 0u;              // as the next call expects it
+      }
+    }
+    start += rt.n;
+    if (start >= end) return;
+    if (++row == rows) {
+      row = 0;
+      ++seq;
+      rt = tiles_of(seq);
+    }
+  }
+}
+
 template <class M, int QT, bool RUNS>
 __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged_kernel(PagedArgs a) {
   constexpr int W = RUNS ? kRunWaves : kLineWaves, NT = 64 * W;
   constexpr int TT = M::kTokens, NM = M::kMine;
   __shared__ JoinSpace<W, RUNS ? kRunGroups : kLineGroups> sh;
-  __shared__ int scan[2][W], found[2];
+  __shared__ int scan[2][W], found[W][2];
   __shared__ unsigned arrived;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int block = (int)blockIdx.x, grid = (int)gridDim.x;
   const int rows = a.n_kv_heads * a.hg;            // of a sequence
+  // Part slots, Partial [slot_heads] each, stored and loaded where every compute unit sees them.
+  const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, kPartsBytes, kRsrcWord3);
 
   auto length = [&](int b) { return min(max(a.seq_len[b], 0), a.len_max); };
   auto tiles_of = [&](int b) { return row_tiles(length(b), a.window, a.sink, TT); };
@@ -496,18 +764,22 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
     }
     total = __builtin_amdgcn_readfirstlane(total);
     longest = __builtin_amdgcn_readfirstlane(longest);
-    if (rows_whole(longest, a.batch * rows, grid)) {
+    const LineWay way = line_way(total, longest, a.batch * rows, grid, W);
+    quota = way.quota;
+    if (way.waves) {
+      line_of_waves<M, QT>(a, way, total, incl - mine, mine, b0, found, slots);
+      return;
+    }
+    if (way.whole) {
       if (block >= a.batch * rows) return;         // (uniform)
       seq = block / rows;
       row = block % rows;
       rt = tiles_of(seq);
-      quota = longest;
       start = block * quota;
       end = start + rt.n;
       first = 0;
       last = rt.n;
     } else {
-      quota = quota_of(total, grid, W);
       const int begin = block * quota;
       if (begin >= total) return;                  // (uniform)
       end = min(begin + quota, total);
@@ -519,12 +791,12 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
           if (begin < at + t) break;
           at += t;
         }
-        found[0] = b;
-        found[1] = at;
+        found[0][0] = b;
+        found[0][1] = at;
       }
       __syncthreads();
-      seq = __builtin_amdgcn_readfirstlane(found[0]);
-      const int before = __builtin_amdgcn_readfirstlane(found[1]);
+      seq = __builtin_amdgcn_readfirstlane(found[0][0]);
+      const int before = __builtin_amdgcn_readfirstlane(found[0][1]);
       rt = tiles_of(seq);
       row = (begin - before) / rt.n;
       start = before + row * rt.n;
@@ -537,138 +809,31 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
   }
 
   for (;;) {
-    const int len = length(seq);
-    const int lo = a.window > 0 ? max(0, len - a.window) : 0;
-    const int kvh = row / a.hg, h0 = kvh * a.G + (row % a.hg) * kPagedHeads;
-    const int heads = min(kPagedHeads, (kvh + 1) * a.G - h0);
-    const int64_t q_row = (int64_t)seq * a.n_q_heads + h0;
-    const int32_t* table = a.table + seq * a.table_stride;
-    const char* kb = a.k + kvh * a.head_stride;
-    const char* vb = a.v + kvh * a.head_stride;
-
-    // Page of the 8-token block `blk` of the tile at token t0 (-1: none there).
-    auto page_of = [&](int t0, int blk) {
-      const int i = (t0 + 8 * blk) >> a.page_shift;
-      return i < a.max_pages ? table[i] : -1;
-    };
-    auto exists = [&](int page) { return (page >= 0) & (page < a.n_pages); };
-    const int slot_mask = (1 << a.page_shift) - 1;
-    auto key_row = [&](int t0, int page) {
-      const int t = t0 + M::key_token(0, n);
-      return kb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
-    };
-    auto value_row = [&](int t0, int page) {
-      const int t = t0 + NM * g;
-      return vb + (exists(page) ? page : 0) * a.page_stride + (t & slot_mask) * a.tok_stride;
-    };
-
-    // Two tiles ahead: pages; one tile ahead: keys and values.
-    int i = first + wave;
-    int t0 = rt.token(min(i, last - 1), TT), t1 = rt.token(min(i + W, last - 1), TT);
-    int kp = page_of(t0, M::key_block(n)), vp = page_of(t0, M::value_block(g));
-    int kp1 = page_of(t1, M::key_block(n)), vp1 = page_of(t1, M::value_block(g));
-    typename M::template Query<QT> q;
-    q.load(a.q, a.q_dtype, (int64_t)seq * a.q_stride + (int64_t)(h0 + min(n, heads - 1)) * kD,
-           n < heads, g);
-    const float slope = a.slopes && n < heads ? a.slopes[h0 + n] * kLog2e : 0.f;
-
-    float m_run = -INFINITY, l_run = 0.f;
-    v4f acc[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
-    typename M::Keys key;
-    typename M::Values val;
-    if (i < last) {
-      key.load(key_row(t0, kp), a.tok_stride, g);
-      val.load(value_row(t0, vp), a.tok_stride, n);
-    }
-    for (; i < last; i += W) {
-      const bool more = i + W < last;
-      float z[NM];
-      M::template scores<QT>(key, q, z);
-      if (more) key.load(key_row(t1, kp1), a.tok_stride, g);
-      const int t2 = rt.token(min(i + 2 * W, last - 1), TT);
-      const int kp2 = page_of(t2, M::key_block(n)), vp2 = page_of(t2, M::value_block(g));
-      if (a.cap > 0.f) {
-        const float in = a.scale / a.cap, out = a.cap * kLog2e;
-#pragma unroll
-        for (int e = 0; e < NM; ++e) z[e] = out * tanh_of(z[e] * in);
-      } else {
-#pragma unroll
-        for (int e = 0; e < NM; ++e) z[e] *= a.scale * kLog2e;
-      }
-      if (a.slopes) {
-#pragma unroll
-        for (int e = 0; e < NM; ++e) z[e] -= slope * (float)(len - 1 - (t0 + NM * g + e));
-      }
-      // A tile that is attended as a whole needs no masks.
-      const bool there = exists(vp);
-      const bool whole = t0 + TT <= len && (t0 >= lo || t0 + TT <= a.sink) &&
-                         __builtin_amdgcn_ballot_w64(!there) == 0;
-      if (!whole) {
-#pragma unroll
-        for (int e = 0; e < NM; ++e) {
-          const int t = t0 + NM * g + e;
-          // (no short circuits: selects, not branches)
-          const bool on = there & (t < len) & ((t >= lo) | (t < a.sink));
-          z[e] = on ? z[e] : -INFINITY;
-          val.keep(e, on);
-        }
-      }
-      float m = z[0];
-#pragma unroll
-      for (int e = 1; e < NM; ++e) m = fmaxf(m, z[e]);
-      m = fmaxf(m_run, over_groups_max(m) - M::kLower);
-      const float ref = m == -INFINITY ? 0.f : m;
-      const float sa = __builtin_amdgcn_exp2f(m_run - ref);      // (0 at the first tile)
-      float p[NM], sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < NM; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
-        sum += p[e];
-      }
-      l_run = l_run * sa + sum;
-      m_run = m;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] *= sa;
-      M::accumulate(val, p, acc);
-      if (more) val.load(value_row(t1, vp1), a.tok_stride, n);
-      t0 = t1, vp = vp1;
-      t1 = t2, kp1 = kp2, vp1 = vp2;
-    }
-    l_run = over_groups_sum(l_run);
+    const Row r = row_of(a, seq, row);
+    const int heads = r.heads;
+    RowPart mine;
+    attend<M, QT>(a, seq, r, rt, first + wave, last, W, mine);
 
     // The waves' parts meet in LDS.
     if (g == 0) {
-      sh.m[wave][n] = m_run;
-      sh.l[wave][n] = l_run;
+      sh.m[wave][n] = mine.m;
+      sh.l[wave][n] = mine.l;
     }
     if (n < heads) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sh.sums[wave][n][M::channel(j, r, g)] = acc[j][r];
+        for (int i = 0; i < 4; ++i) sh.sums[wave][n][M::channel(j, i, g)] = mine.acc[j][i];
     }
     __syncthreads();
 
-    // What a row ends as: outputs and log-sum-exp, or a partial for another join.
     auto finish = [&](int h, int c4, float m, float l, v4f o) {
-      if (a.seg) {
-        Partial* s = a.seg + q_row + h;
-        reinterpret_cast<v4f*>(s->o)[c4] = o;
-        if (c4 == 0) *reinterpret_cast<v4f*>(s) = (v4f){m, l, 0.f, 0.f};
-        return;
-      }
-      const v4f zero = {0.f, 0.f, 0.f, 0.f};
-      reinterpret_cast<v4f*>(a.out)[(q_row + h) * (kD / 4) + c4] = l == 0.f ? zero : o / l;
-      if (a.lse && c4 == 0) a.lse[q_row + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      finish_row(a, r.q_row + h, c4, m, l, o);
     };
-    // Part slots: Partial [kPagedHeads], stored and loaded where every compute unit sees them.
-    const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, kPartsBytes, kRsrcWord3);
     auto part_at = [&](int p, int h) {
       const int w = block - part + p;
       const int slot = RUNS ? w : part_slot(w, start, quota);
-      return (slot * kPagedHeads + h) * (int)sizeof(Partial);
+      return (slot * a.slot_heads + h) * (int)sizeof(Partial);
     };
     for (int x = tid; x < heads * (kD / 4); x += NT) {
       const int h = x / (kD / 4), c4 = x % (kD / 4);
@@ -733,18 +898,18 @@ size_t counters_bytes(int batch, int n_q_heads, int n_kv_heads) {
 }  // namespace
 
 size_t paged_workspace_bytes(int batch, int n_q_heads, int n_kv_heads) {
-  return counters_bytes(batch, n_q_heads, n_kv_heads) + kPartsBytes;
+  return kPartsBytes + counters_bytes(batch, n_q_heads, n_kv_heads);
 }
 
 aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
-  a.counters = static_cast<unsigned*>(workspace);
-  a.parts = reinterpret_cast<Partial*>(static_cast<char*>(workspace) +
-                                       counters_bytes(a.batch, a.n_q_heads, a.n_kv_heads));
+  a.parts = static_cast<Partial*>(workspace);
+  a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kPartsBytes);
   const int tt = c_dtype == AATC_F32 ? Full32::kTokens : Half16<__bf16>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
   if (most > (1 << 30)) return AATC_E_UNSUPPORTED;
   const bool runs = rows <= kMaxRunRows;
+  a.slot_heads = std::min(a.G, kPagedHeads);
   const int grid = (int)std::min<int64_t>(runs ? kRunGroups : kLineGroups, most);
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](auto kernel) {

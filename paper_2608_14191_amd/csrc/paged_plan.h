@@ -62,26 +62,36 @@ AATC_PAGED_HD inline int runs_of(int n, int q) { return (n + q - 1) / q; }
 // Run i of `runs` has the row's tiles from here on.
 AATC_PAGED_HD inline int run_begin(int n, int runs, int i) { return (int)((int64_t)n * i / runs); }
 
-// Lines, for many rows: the tiles of all rows lie in one line, row after row; workgroup w takes
-// those from w quota on, of several rows or of a part of one.  Rows so short that one workgroup
-// has each in a few rounds of its waves are not cut if there is a workgroup for every row.
-constexpr int kWholeRow = 32;
-AATC_PAGED_HD inline bool rows_whole(int longest, int rows, int grid) {
-  return longest <= kWholeRow && rows <= grid;
+// Lines, for many rows: the tiles of all rows lie in one line, row after row; worker w (a wave for
+// itself, or a workgroup whose waves share rows) takes those from w quota on, of several rows or
+// of a part of one.  Or whole rows: a worker has one row (quota is then the longest).
+//
+// To begin a row, and to join its parts, takes a wave about as long as five tiles each.  So rows
+// stay whole, a wave each, where there are waves enough and the longest is not much over the
+// average share (1544 rows of 13 tiles at most: 68 us shared by workgroups), or a workgroup each.
+// Else waves for themselves, unless rows would be cut into many parts (784 rows of 60 tiles at
+// most: 126 us by waves, 114 by workgroups).
+struct LineWay {
+  int quota;
+  bool waves, whole;
+};
+AATC_PAGED_HD inline LineWay line_way(int tiles, int longest, int rows, int groups, int waves) {
+  const int all = groups * waves, share = (tiles + all - 1) / all;
+  if (rows <= all && longest <= share + 8) return {longest, true, true};
+  if (rows <= groups && longest <= 8 * waves) return {longest, false, true};
+  const int q = share > 4 ? share : 4;
+  if (longest <= 3 * q) return {q, true, false};
+  const int even = (tiles + groups - 1) / groups;
+  return {even > waves ? even : waves, false, false};
 }
-// Else: tiles of a workgroup, one for each of its waves at least.
-AATC_PAGED_HD inline int quota_of(int tiles, int grid, int waves) {
-  const int even = (tiles + grid - 1) / grid;
-  return even > waves ? even : waves;
-}
-// A row that starts at `start` with n tiles is shared by the workgroups first .. last.
+// A row that starts at `start` with n tiles is shared by the workers first .. last.
 struct RowShare {
   int first, last;
 };
 AATC_PAGED_HD inline RowShare row_share(int start, int n, int quota) {
   return {start / quota, (start + n - 1) / quota};
 }
-// The workspace slot of workgroup w's part of that row: one for a row that it goes on with, one
+// The workspace slot of worker w's part of that row: one for a row that it goes on with, one
 // for a row that it begins.
 AATC_PAGED_HD inline int part_slot(int w, int start, int quota) {
   return 2 * w + (start >= w * quota ? 1 : 0);

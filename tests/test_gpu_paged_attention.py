@@ -167,6 +167,17 @@ def test_query_stride_and_workspace_reuse():
     assert (b.double() - want).norm() <= 2e-6 * want.norm()
 
 
+def test_workspace_of_calls_of_other_shapes():
+    """One workspace, large enough for all: few rows and many, few heads and many, in turn."""
+    cases = [_case(20, [900] * 3, 16, 1, 16), _case(21, [40, 300, 90] * 50, 2, 1, 16),
+             _case(22, [5000], 32, 8, 16), _case(23, [20, 2600] * 12, 12, 12, 16)]
+    ws = torch.zeros(max(P.aatc_paged_decode_workspace_bytes(c[4].shape[0], c[4].shape[1], c[0].shape[1])
+                         for c in cases), dtype=torch.uint8, device="cuda")
+    want = [_run(*c)[0] for c in cases]
+    for i in (0, 1, 2, 3, 1, 0, 3, 2, 1):
+        assert torch.equal(_run(*cases[i], workspace=ws)[0], want[i]), i
+
+
 def test_non_finite_queries_and_values():
     k, v, table, lens, q = _case(11, [50, 50], 4, 2, 16)
     q[0, 1, 3] = NAN
