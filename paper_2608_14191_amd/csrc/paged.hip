@@ -953,7 +953,6 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   const int tt = c_dtype == AATC_F32 ? Full32::kTokens : Half16<__bf16>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
-  if (most > (1 << 30)) return AATC_E_UNSUPPORTED;
   const bool runs = rows <= kMaxRunRows;
   a.slot_heads = std::min(a.G, kPagedHeads);
   const int grid = (int)std::min<int64_t>(runs ? kRunGroups : kLineGroups, most);

@@ -66,6 +66,12 @@ int64_t row_tokens(const aatc_page_table& t, int page_tokens) {
   return std::min<int64_t>((int64_t)t.max_pages * page_tokens, INT32_MAX - 4096);
 }
 
+// The plan of the attention counts tiles (16 tokens at least) in 32 bits.
+bool too_many_tiles(const aatc_paged_cache& c, const aatc_page_table& t, int64_t batch, int hq) {
+  const int64_t hg = (hq / c.n_kv_heads + 15) / 16;
+  return (row_tokens(t, c.page_tokens) / 16 + 1) > kMaxList / (batch * c.n_kv_heads * hg);
+}
+
 aatc_status check_counts(const int32_t* ref, int64_t n_pages) {
   return ref && aligned(ref, 4) && n_pages >= 1 && n_pages <= kMaxPages ? AATC_OK
                                                                         : AATC_E_INVALID;
@@ -264,6 +270,7 @@ extern "C" aatc_status aatc_paged_decode_attention(
     if (!out || !aligned(out, 16) || !aligned(lse, 4) || !aligned(slopes, 4) || !workspace ||
         !aligned(workspace, 256))
       return AATC_E_INVALID;
+    if (too_many_tiles(*cache, *table, batch, n_q_heads)) return AATC_E_UNSUPPORTED;
     if (ws_bytes < paged_workspace_bytes(batch, n_q_heads, cache->n_kv_heads))
       return AATC_E_WORKSPACE;
     PagedArgs a = paged_args(*cache, *table, seq_len, batch, n_q_heads, q, q_dtype, q_stride,
@@ -309,6 +316,7 @@ extern "C" aatc_status aatc_decode_attention_paged(
                      k_codes, k_alpha, v_codes, v_alpha, seq_len, cap, k_record_bytes,
                      v_record_bytes, softmax_scale, out, workspace, ws_bytes);
     if (e != AATC_OK) return e;
+    if (too_many_tiles(*cache, *table, batch, n_q_heads)) return AATC_E_UNSUPPORTED;
     if (ws_bytes < own + paged_workspace_bytes(batch, n_q_heads, n_kv_heads))
       return AATC_E_WORKSPACE;
     const PagedArgs a = paged_args(*cache, *table, page_len, batch, n_q_heads, q, q_dtype,
