@@ -15,7 +15,9 @@ namespace {
 
 constexpr int kListThreads = 256;
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr int kPlanPages = 16;                  // pages per thread and step of a scan
+// Pages per thread and step of a scan: four where one step has the whole pool then (all waves share
+// it), else sixteen (fewer steps).
+constexpr int kFewPages = 4, kManyPages = 16;
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
@@ -40,6 +42,42 @@ __device__ inline int block_scan(int v, int& sum, int* scratch) {
   __syncthreads();
   sum = all;
   return before + incl - v;
+}
+
+// The pages of a step, in order: wave, then k, then lane (64 consecutive ones an access).
+template <int PP>
+__device__ inline int64_t plan_page(int64_t base, int k) {
+  return base + (int64_t)(threadIdx.x >> 6) * (64 * PP) + k * 64 + (threadIdx.x & 63);
+}
+
+// Marked pages of a step (flag(k)): calls take(rank, k) for each of this thread's, ranks counted
+// from `first` in the pages' order, and returns how many the workgroup has.  Two barriers.
+template <int PP, class Flag, class Take>
+__device__ inline int rank_pages(int first, int* scratch, Flag flag, Take take) {
+  const int wave = threadIdx.x >> 6;
+  uint64_t marks[PP];
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < PP; ++k) {
+    marks[k] = __builtin_amdgcn_ballot_w64(flag(k));
+    mine += __popcll(marks[k]);
+  }
+  if ((threadIdx.x & 63) == 0) scratch[wave] = mine;
+  __syncthreads();
+  int before = first, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    before += w < wave ? scratch[w] : 0;
+    all += scratch[w];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PP; ++k) {
+    const uint64_t bit = (uint64_t)1 << (threadIdx.x & 63);
+    if (marks[k] & bit) take(before + __popcll(marks[k] & (bit - 1)), k);
+    before += __popcll(marks[k]);
+  }
+  return all;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -78,8 +116,10 @@ __global__ __launch_bounds__(kListThreads) void free_kernel(int32_t* table, int6
 }
 
 // ---------------------------------------------------------------------------------------
-// Reserve: one workgroup.  Workspace: for every row the first of its places in the list of free
-// pages to hand out, its partial page to leave (-1: none), then that list.
+// Reserve: one workgroup.  For every row the first of its places in the list of free pages to hand
+// out and its partial page to leave (-1: none), and that list, are in LDS as far as they fit (the
+// round trips to memory are the time: 128 children of 32 parents 12.0 us with all of them in the
+// workspace), else in the workspace.
 struct ReserveSpace {
   int32_t *place, *leave, *free;
 };
@@ -87,15 +127,21 @@ __host__ __device__ inline ReserveSpace reserve_space(void* ws, int64_t rows) {
   auto* p = static_cast<int32_t*>(ws);
   return {p, p + rows, p + 2 * rows};
 }
+constexpr int kFreeLds = 2048;
 
+template <int PP>
 __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
-    int32_t* table, int64_t stride, int rows, int entries, int32_t* ref, int n_pages, int shift,
-    int len_max, const int32_t* __restrict__ held, const int32_t* __restrict__ wanted,
-    int32_t* pairs, int32_t* lacking, void* ws) {
+    int32_t* table, int64_t stride, int rows, int32_t* ref, int n_pages, int shift, int len_max,
+    const int32_t* __restrict__ held, const int32_t* __restrict__ wanted, int32_t* pairs,
+    int32_t* lacking, void* ws) {
   __shared__ int scratch[kPlanWaves];
-  __shared__ int chunk[kPlanThreads];
+  __shared__ int chunk[kPlanThreads], place_s[kPlanThreads], leave_s[kPlanThreads], free_s[kFreeLds];
   const int tid = threadIdx.x;
   const ReserveSpace sp = reserve_space(ws, rows);
+  const bool small = rows <= kPlanThreads;
+  auto place_of = [&](int r) { return small ? place_s[r] : sp.place[r]; };
+  auto leave_of = [&](int r) { return small ? leave_s[r] : sp.leave[r]; };
+  auto free_page = [&](int i) { return i < kFreeLds ? free_s[i] : sp.free[i]; };
   const int mask = (1 << shift) - 1;
   // Row r: tokens from .. to - 1 to come.
   struct Row {
@@ -114,6 +160,17 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
   auto new_pages = [&](const Row& w) {
     return w.grows() ? ((w.to + mask) >> shift) - ((w.from + mask) >> shift) : 0;
   };
+  // The free ones of this thread's pages of a step, a bit each (the first step's are read now).
+  auto open_pages = [&](int64_t base) {
+    unsigned open = 0;
+#pragma unroll
+    for (int k = 0; k < PP; ++k) {
+      const int64_t p = plan_page<PP>(base, k);
+      if (p < n_pages && ref[p] <= 0) open |= 1u << k;
+    }
+    return open;
+  };
+  const unsigned open0 = open_pages(0);
   // (1) What each row needs: a page in the place of one that others hold too, unless every other
   // holder is an earlier row of this call that gets a copy, and its new pages.
   int demand = 0;
@@ -126,52 +183,47 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     if (__syncthreads_or(count > 1)) {
       for (int b = 0; b <= base; b += kPlanThreads) {
         const int other = b + tid;
-        int page = -1;
-        if (b == base) page = mine;
-        else page = partial_of(other, row_of(other));
+        const int page = b == base ? mine : partial_of(other, row_of(other));
         __syncthreads();
         chunk[tid] = page;
         __syncthreads();
         if (count > 1) {
           const int upto = b == base ? tid : kPlanThreads;
+#pragma unroll 8
           for (int k = 0; k < upto; ++k) earlier += chunk[k] == mine;
         }
       }
     }
     const bool copy = count - earlier > 1;
     int sum = 0;
-    const int place = block_scan((copy ? 1 : 0) + new_pages(w), sum, scratch);
+    const int place = demand + block_scan((copy ? 1 : 0) + new_pages(w), sum, scratch);
     if (r < rows) {
-      sp.place[r] = demand + place;
-      sp.leave[r] = copy ? mine : -1;
+      (small ? place_s : sp.place)[r] = place;
+      (small ? leave_s : sp.leave)[r] = copy ? mine : -1;
     }
     demand += sum;
   }
   // (2) The lowest free pages, as many.
   int found = 0;
-  for (int64_t base = 0; base < n_pages && found < demand; base += kPlanThreads * kPlanPages) {
-    const int64_t p0 = base + tid * kPlanPages;
-    unsigned open = 0;
-#pragma unroll
-    for (int k = 0; k < kPlanPages; ++k)
-      if (p0 + k < n_pages && ref[p0 + k] <= 0) open |= 1u << k;
-    int sum = 0;
-    int place = found + block_scan(__popc(open), sum, scratch);
-    while (open && place < demand) {
-      sp.free[place++] = (int)p0 + __builtin_ctz(open);
-      open &= open - 1;
-    }
-    found += sum;
+  for (int64_t base = 0; base < n_pages && found < demand; base += kPlanThreads * PP) {
+    const unsigned open = base == 0 ? open0 : open_pages(base);
+    found += rank_pages<PP>(found, scratch, [&](int k) { return (open >> k & 1u) != 0u; },
+                        [&](int rank, int k) {
+                          if (rank >= demand) return;
+                          const int page = (int)plan_page<PP>(base, k);
+                          if (rank < kFreeLds) free_s[rank] = page;
+                          else sp.free[rank] = page;
+                        });
   }
   __syncthreads();                              // (the list is this workgroup's own)
   const bool enough = found >= demand;
   if (tid == 0) *lacking = enough ? 0 : demand - found;
   // (3) Hand out.
   for (int r = tid; r < rows; r += kPlanThreads) {
-    const int old = enough ? sp.leave[r] : -1;
+    const int old = enough ? leave_of(r) : -1;
     int now = -1;
     if (old >= 0) {
-      now = sp.free[sp.place[r]];
+      now = free_page(place_of(r));
       table[r * stride + (row_of(r).from >> shift)] = now;
       atomicAdd(&ref[old], -1);
       ref[now] = 1;
@@ -184,12 +236,12 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     int lo = 0, hi = rows - 1;                  // the last row whose places begin at or before i
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
-      if (sp.place[mid] <= i) lo = mid;
+      if (place_of(mid) <= i) lo = mid;
       else hi = mid - 1;
     }
-    const int k = i - sp.place[lo] - (sp.leave[lo] >= 0 ? 1 : 0);
+    const int k = i - place_of(lo) - (leave_of(lo) >= 0 ? 1 : 0);
     if (k < 0) continue;                        // the copy's
-    const int page = sp.free[i];
+    const int page = free_page(i);
     table[lo * stride + ((row_of(lo).from + mask) >> shift) + k] = page;
     ref[page] = 1;
   }
@@ -198,56 +250,46 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
 // ---------------------------------------------------------------------------------------
 // Compact: where each page goes (one workgroup), then the table (all of them).  Workspace: the
 // new place of every page.
+template <int PP>
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const int32_t* ref,
                                                                     int n_pages, int32_t* ref_out,
                                                                     int32_t* pairs,
                                                                     int32_t* moves, int32_t* to) {
   __shared__ int scratch[kPlanWaves];
   const int tid = threadIdx.x;
-  constexpr int kStep = kPlanThreads * kPlanPages;
+  constexpr int kStep = kPlanThreads * PP;
   int live = 0;
-  for (int64_t base = 0; base < n_pages; base += kStep) {
-    int n = 0;
-#pragma unroll
-    for (int k = 0; k < kPlanPages; ++k) {
-      const int64_t p = base + k * kPlanThreads + tid;
-      n += p < n_pages && ref[p] > 0;
-    }
-    int sum = 0;
-    block_scan(n, sum, scratch);
-    live += sum;
-  }
-  // Pages in use from `live` on, and free ones below it: as many of one as of the other.
+  for (int64_t base = 0; base < n_pages; base += kStep)
+    live += rank_pages<PP>(0, scratch, [&](int k) {
+      const int64_t p = plan_page<PP>(base, k);
+      return p < n_pages && ref[p] > 0;
+    }, [](int, int) {});
+  // Pages in use from `live` on, and free ones below it: as many of one as of the other.  (ref_out
+  // may be ref: no count is written before all of its own step are read.)
   int movers = 0, holes = 0;
   for (int64_t base = 0; base < n_pages; base += kStep) {
-    const int64_t p0 = base + (int64_t)tid * kPlanPages;
-    unsigned go = 0, open = 0;
+    int count[PP];
 #pragma unroll
-    for (int k = 0; k < kPlanPages; ++k) {
-      const int64_t p = p0 + k;
-      if (p >= n_pages) continue;
-      const bool used = ref[p] > 0;
-      go |= (used && p >= live) ? 1u << k : 0u;
-      open |= (!used && p < live) ? 1u << k : 0u;
-      to[p] = (int)p;
+    for (int k = 0; k < PP; ++k) {
+      const int64_t p = plan_page<PP>(base, k);
+      count[k] = p < n_pages ? ref[p] : 0;
     }
-    int sum = 0;
-    int at = movers + block_scan(__popc(go), sum, scratch);
-    movers += sum;
-    for (; go; go &= go - 1) pairs[2 * at++] = (int)p0 + __builtin_ctz(go);
-    at = holes + block_scan(__popc(open), sum, scratch);
-    holes += sum;
-    for (; open; open &= open - 1) pairs[2 * at++ + 1] = (int)p0 + __builtin_ctz(open);
+#pragma unroll
+    for (int k = 0; k < PP; ++k) {
+      const int64_t p = plan_page<PP>(base, k);
+      if (p >= n_pages) continue;
+      to[p] = (int)p;
+      if (ref_out != ref) ref_out[p] = p < live ? count[k] : 0;
+    }
+    movers += rank_pages<PP>(movers, scratch, [&](int k) {
+      return count[k] > 0 && plan_page<PP>(base, k) >= live;
+    }, [&](int rank, int k) { pairs[2 * rank] = (int)plan_page<PP>(base, k); });
+    holes += rank_pages<PP>(holes, scratch, [&](int k) {
+      return count[k] <= 0 && plan_page<PP>(base, k) < live;
+    }, [&](int rank, int k) { pairs[2 * rank + 1] = (int)plan_page<PP>(base, k); });
   }
   __syncthreads();
   if (tid == 0) *moves = movers;
-  // (ref_out may be ref: counts are read before any of them is written.)
-  for (int64_t base = 0; base < n_pages; base += kPlanThreads) {
-    const int64_t p = base + tid;
-    if (p < n_pages && p >= live && ref_out != ref) ref_out[p] = 0;
-    if (p < live && ref_out != ref) ref_out[p] = ref[p];
-  }
-  __syncthreads();
   for (int64_t i = tid; i < n_pages / 2; i += kPlanThreads) {
     if (i < movers) {
       const int from = pairs[2 * i], dst = pairs[2 * i + 1];
@@ -351,9 +393,10 @@ aatc_status launch_pages_reserve(const aatc_page_table& t, int32_t* ref, int64_t
                                  int32_t* pairs, int32_t* lacking, void* workspace, void* stream) {
   const int64_t most = (int64_t)t.max_pages * page_tokens;
   const int len_max = (int)std::min<int64_t>(most, INT32_MAX - kMaxPage);
-  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, (hipStream_t)stream, t.table,
-                     t.stride, t.rows, t.max_pages, ref, (int)n_pages, log2_of(page_tokens),
-                     len_max, held, wanted, pairs, lacking, workspace);
+  const bool few = n_pages <= kPlanThreads * kFewPages;
+  hipLaunchKernelGGL(few ? reserve_kernel<kFewPages> : reserve_kernel<kManyPages>, dim3(1),
+                     dim3(kPlanThreads), 0, (hipStream_t)stream, t.table, t.stride, t.rows, ref,
+                     (int)n_pages, log2_of(page_tokens), len_max, held, wanted, pairs, lacking, workspace);
   return done();
 }
 
@@ -362,7 +405,8 @@ aatc_status launch_pages_compact(const aatc_page_table& t, const int32_t* ref, i
                                  int32_t* moves, void* workspace, void* stream) {
   const hipStream_t st = (hipStream_t)stream;
   auto* to = static_cast<int32_t*>(workspace);
-  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, ref, (int)n_pages,
+  const bool few = n_pages <= kPlanThreads * kFewPages;
+  hipLaunchKernelGGL(few ? compact_plan_kernel<kFewPages> : compact_plan_kernel<kManyPages>, dim3(1), dim3(kPlanThreads), 0, st, ref, (int)n_pages,
                      ref_out, pairs, moves, to);
   if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
   const int64_t all = (int64_t)t.rows * t.max_pages;
