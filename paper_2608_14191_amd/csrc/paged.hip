@@ -89,8 +89,18 @@ __device__ inline void load_queries(const void* q, int dtype, int64_t i, bool on
   }
 }
 
+// FAR: keys and values are loaded past the caches.  Pools that do not fit there have nothing to
+// gain from them (4 x 131072 tokens, 8 KV heads: 323 us, 362 through the caches; 1 x 32768 28.8
+// and 31.8), smaller ones may be found there again (1 x 4000 tokens 14.4 and 12.8).
+constexpr int64_t kFarBytes = (int64_t)128 << 20;
+template <bool FAR, class V>
+__device__ inline V load16(const char* p) {
+  if constexpr (FAR) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+
 // The two products on 16-bit types.  A lane's place: n = lane % 16, g = lane / 16.
-template <class T>
+template <class T, bool FAR>
 struct Half16 {
   static constexpr bool kF16 = sizeof(T) == 2 && __is_same(T, _Float16);
   typedef T v8 __attribute__((ext_vector_type(8)));
@@ -162,7 +172,7 @@ struct Half16 {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
-          r[u][kk] = *reinterpret_cast<const v4u*>(row0 + u * 4 * tok_stride + 64 * kk + 16 * g);
+          r[u][kk] = load16<FAR, v4u>(row0 + u * 4 * tok_stride + 64 * kk + 16 * g);
     }
   };
   struct Values {
@@ -170,7 +180,7 @@ struct Half16 {
     __device__ void load(const char* row0, int64_t tok_stride, int n) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        r[e] = *reinterpret_cast<const v4u*>(row0 + e * tok_stride + 16 * n);
+        r[e] = load16<FAR, v4u>(row0 + e * tok_stride + 16 * n);
     }
     // Token e of the lane's counts as zeros unless `on` (0 times what is stored there may be NaN).
     __device__ void keep(int e, bool on) {
@@ -221,6 +231,7 @@ struct Half16 {
 };
 
 // The two products on float32 (v_mfma_f32_16x16x4_f32: no splitting).
+template <bool FAR>
 struct Full32 {
   static constexpr int kTokens = 16;
   static constexpr int kMine = 4;                 // tokens 4 g .. 4 g + 3
@@ -247,7 +258,7 @@ struct Full32 {
     v4f r[8];
     __device__ void load(const char* row0, int64_t, int g) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) r[c] = *reinterpret_cast<const v4f*>(row0 + 64 * c + 16 * g);
+      for (int c = 0; c < 8; ++c) r[c] = load16<FAR, v4f>(row0 + 64 * c + 16 * g);
     }
   };
   struct Values {
@@ -257,7 +268,7 @@ struct Full32 {
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-          r[e][c] = *reinterpret_cast<const v4f*>(row0 + e * tok_stride + 256 * c + 16 * n);
+          r[e][c] = load16<FAR, v4f>(row0 + e * tok_stride + 256 * c + 16 * n);
     }
     __device__ void keep(int e, bool on) {
 #pragma unroll
@@ -950,7 +961,7 @@ size_t paged_workspace_bytes(int batch, int n_q_heads, int n_kv_heads) {
 aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
   a.parts = static_cast<Partial*>(workspace);
   a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kPartsBytes);
-  const int tt = c_dtype == AATC_F32 ? Full32::kTokens : Half16<__bf16>::kTokens;
+  const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
   const bool runs = rows <= kMaxRunRows;
@@ -970,13 +981,21 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   using One = std::integral_constant<int, 1>;
   using Three = std::integral_constant<int, 3>;
   const bool same = a.q_dtype == (int)c_dtype;
-  switch (c_dtype) {
-    case AATC_F32: return launch_as(Full32{}, One{});
-    case AATC_BF16:
-      return same ? launch_as(Half16<__bf16>{}, One{}) : launch_as(Half16<__bf16>{}, Three{});
-    default:
-      return same ? launch_as(Half16<_Float16>{}, One{}) : launch_as(Half16<_Float16>{}, Three{});
-  }
+  auto launch_type = [&](auto far) {
+    constexpr bool F = decltype(far)::value;
+    switch (c_dtype) {
+      case AATC_F32: return launch_as(Full32<F>{}, One{});
+      case AATC_BF16:
+        return same ? launch_as(Half16<__bf16, F>{}, One{}) : launch_as(Half16<__bf16, F>{}, Three{});
+      default:
+        return same ? launch_as(Half16<_Float16, F>{}, One{})
+                    : launch_as(Half16<_Float16, F>{}, Three{});
+    }
+  };
+  const int64_t page_bytes = ((int64_t)1 << a.page_shift) * a.n_kv_heads * kD *
+                             (c_dtype == AATC_F32 ? 4 : 2);
+  const bool far = 2 * page_bytes > kFarBytes / a.n_pages;       // (both pools)
+  return far ? launch_type(std::true_type{}) : launch_type(std::false_type{});
 }
 
 }  // namespace aatc
