@@ -38,7 +38,7 @@ namespace {
 // other (48 x 2052 tokens, 8 KV heads, float32: 144.5 us, with eight waves 159.9).
 constexpr int kRunWaves = 8, kRunGroups = 256;
 constexpr int kLineWaves = 4, kLineGroups = 512;
-constexpr int kMaxRunRows = 128;                  // two sequences a lane (every row counts one)
+constexpr int kMaxRunRows = 256;                  // a workgroup each at least
 constexpr int kPagedHeads = 16;                   // query heads of a row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The workspace: part slots, two a wave of the lines, then the counters.  (The slots' size is fixed
@@ -740,39 +740,57 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
     const int all = a.batch * rows;
     if (a.batch == 1) {
       rt = tiles_of(0);
-      parts = runs_of(rt.n, W * smallest_rounds(rt.n * rows, rows, grid, W, [&](int q) {
+      parts = runs_of(rt.n, W * smallest_rounds(rt.n * rows, rt.n, rows, grid, W, [&](int q) {
                         return rows * runs_of(rt.n, q);
                       }));
       row = block / parts;
       part = block % parts;
       if (row >= rows) return;                     // (uniform)
     } else {
-      // Two sequences a lane; every wave does the same.
-      const int n0 = lane < a.batch ? tiles_of(lane).n : 0;
-      const int n1 = lane + 64 < a.batch ? tiles_of(lane + 64).n : 0;
-      auto sum_of = [&](int v) {
+      // Some sequences a lane; every wave does the same.
+      constexpr int S = kMaxRunRows / 64;
+      int n_of[S], longest = 0, tiles = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-        return __builtin_amdgcn_readfirstlane(v);
-      };
-      const int q = W * smallest_rounds(sum_of(n0 + n1) * rows, all, grid, W, [&](int x) {
-                      return rows * sum_of(runs_of(n0, x) + runs_of(n1, x));
-                    });
-      const int r0 = rows * runs_of(n0, q), r1 = rows * runs_of(n1, q);
-      int i0 = r0, i1 = r1;                        // inclusive sums in the sequences' order
+      for (int i = 0; i < S; ++i) {
+        n_of[i] = lane + 64 * i < a.batch ? tiles_of(lane + 64 * i).n : 0;
+        longest = max(longest, n_of[i]);
+        tiles += n_of[i];
+      }
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
-        const int u0 = __shfl_up(i0, o, 64), u1 = __shfl_up(i1, o, 64);
-        i0 += lane >= o ? u0 : 0;
-        i1 += lane >= o ? u1 : 0;
+        tiles += __shfl_xor(tiles, o, 64);
+        longest = max(longest, __shfl_xor(longest, o, 64));
       }
-      i1 += __shfl(i0, 63, 64);
-      if (block >= __builtin_amdgcn_readlane(i1, 63)) return;      // (uniform)
-      // Sequences whose runs all come before this one.
-      seq = __popcll(__builtin_amdgcn_ballot_w64(i0 <= block)) +
-            __popcll(__builtin_amdgcn_ballot_w64(i1 <= block));
-      const int before = seq < 64 ? __builtin_amdgcn_readlane(i0 - r0, seq)
-                                  : __builtin_amdgcn_readlane(i1 - r1, seq - 64);
+      longest = __builtin_amdgcn_readfirstlane(longest);
+      tiles = __builtin_amdgcn_readfirstlane(tiles);
+      const int q = W * smallest_rounds(tiles * rows, longest, all, grid, W, [&](int x) {
+                      int v = 0;
+#pragma unroll
+                      for (int i = 0; i < S; ++i) v += runs_of(n_of[i], x);
+#pragma unroll
+                      for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+                      return rows * __builtin_amdgcn_readfirstlane(v);
+                    });
+      // Runs before each sequence; the one that has this workgroup's, and its first.
+      int carry = 0, before = 0;
+      seq = 0;
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        const int mine = rows * runs_of(n_of[i], q);
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int up = __shfl_up(incl, o, 64);
+          incl += lane >= o ? up : 0;
+        }
+        incl += carry;
+        carry = __builtin_amdgcn_readlane(incl, 63);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(incl <= block);
+        seq += __popcll(past);
+        if (past != ~(uint64_t)0 && carry > block && seq < 64 * (i + 1) && seq >= 64 * i)
+          before = __builtin_amdgcn_readlane(incl - mine, seq - 64 * i);
+      }
+      if (block >= carry) return;                  // (uniform)
       rt = tiles_of(seq);
       parts = runs_of(rt.n, q);
       row = (block - before) / parts;
@@ -964,7 +982,10 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
-  const bool runs = rows <= kMaxRunRows;
+  // Runs for up to half the grid's rows, or up to all of it where no row can be long (one run a row
+  // then lasts as long as the longest: 256 rows up to 2000 tokens 41.1 us, as lines 51.1; 240 rows up
+  // to 12000 tokens 201.7, as lines 161.8).
+  const bool runs = rows <= kRunGroups / 2 || (rows <= kMaxRunRows && a.len_max <= 128 * tt);
   a.slot_heads = std::min(a.G, kPagedHeads);
   const int grid = (int)std::min<int64_t>(runs ? kRunGroups : kLineGroups, most);
   const hipStream_t st = (hipStream_t)stream;

@@ -42,15 +42,20 @@ AATC_PAGED_HD inline RowTiles row_tiles(int len, int window, int sink, int tt) {
 // costs it the latencies of a new start, which few others cover).
 //
 // smallest_rounds: count(q) is the number of runs of at most q tiles, for all rows; `tiles` those
-// of all rows; rows < grid.
+// of all rows, `longest` of one; rows <= grid.
 constexpr int kRoundsMin = 2;         // (a join of parts takes longer than one round more)
 template <class Count>
-AATC_PAGED_HD inline int smallest_rounds(int tiles, int rows, int grid, int waves, Count count) {
+AATC_PAGED_HD inline int smallest_rounds(int tiles, int longest, int rows, int grid, int waves,
+                                         Count count) {
   int lo = (tiles + grid * waves - 1) / (grid * waves);          // the average: none lower fits
   if (lo < kRoundsMin) lo = kRoundsMin;
   if (count(lo * waves) <= grid) return lo;
-  // sum ceil(n / q) <= tiles / q + rows
-  int hi = (tiles + (grid - rows) * waves - 1) / ((grid - rows) * waves);
+  // A run for each row fits; and sum ceil(n / q) <= tiles / q + rows.
+  int hi = (longest + waves - 1) / waves;
+  if (grid > rows) {
+    const int room = (grid - rows) * waves, closed = (tiles + room - 1) / room;
+    hi = closed < hi ? closed : hi;
+  }
   while (hi - lo > 1 + lo / 16) {                                // lo does not fit, hi does
     const int mid = (lo + hi) / 2;
     if (count(mid * waves) <= grid) hi = mid;

@@ -13,9 +13,12 @@ int tiles(int len, int window, int sink, int tt, int* out, int room) {
 }
 
 int rounds(const int* n, int batch, int rows, int grid, int waves) {
-  int tiles = 0;
-  for (int b = 0; b < batch; ++b) tiles += n[b] * rows;
-  return smallest_rounds(tiles, batch * rows, grid, waves, [&](int q) {
+  int tiles = 0, longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    tiles += n[b] * rows;
+    longest = n[b] > longest ? n[b] : longest;
+  }
+  return smallest_rounds(tiles, longest, batch * rows, grid, waves, [&](int q) {
     int c = 0;
     for (int b = 0; b < batch; ++b) c += rows * runs_of(n[b], q);
     return c;
