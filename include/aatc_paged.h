@@ -155,7 +155,7 @@ aatc_status aatc_paged_append(const aatc_paged_cache* cache, const aatc_page_tab
  * q         device, sequence b at q + b * q_stride elements, [n_q_heads][d] contiguous; F32,
  *           BF16 or F16.
  * window    0: none.  sink: tokens at the start that stay attended with a window, >= 0.
- * softcap   0: none, else > 0.
+ * softcap   0: none, else > 0 (and softmax_scale / softcap finite).
  * slopes    device [n_q_heads] fp32 (a bias that falls with distance) or NULL.
  * out       device [batch][n_q_heads][d] fp32, 16-byte aligned.
  * lse       device [batch][n_q_heads] fp32 or NULL.
@@ -208,7 +208,8 @@ aatc_status aatc_decode_attention_paged(
  * (the same or another table, of as many entries per row), and their pages' counts go up: beams
  * and samples share what they have in common.  What the dst rows held is forgotten (not freed).
  * A dst row listed twice takes the last of its sources; rows outside the tables are skipped; no
- * row may be a source and a destination of one call.
+ * row may be a source and a destination of one call.  n < 2^24, as for aatc_pages_free (more:
+ * AATC_E_UNSUPPORTED).
  */
 aatc_status aatc_pages_fork(const aatc_page_table* src, const aatc_page_table* dst, int32_t* ref,
                             int64_t n_pages, const int32_t* pairs, int64_t n, void* stream);
@@ -225,7 +226,7 @@ aatc_status aatc_pages_free(const aatc_page_table* table, int32_t* ref, int64_t 
  * the first of those tokens falls into a page that is already begun and that other entries name
  * too, the row gets a free page of its own for it: pairs[b] = (old, new), for aatc_pages_copy
  * (of rows of one call that share a page to the last entry, the last one keeps it).  pairs[b] =
- * (-1, -1) elsewhere.  Lengths are clamped to [0, max_pages * page_tokens]; wanted[b] <= held[b]
+ * (-1, -1) elsewhere.  A begun page that is not there gets none.  Lengths are clamped to [0, max_pages * page_tokens]; wanted[b] <= held[b]
  * asks for nothing.
  * lacking  device [1] int32: 0, or how many free pages there were too few: then nothing but
  *          lacking and pairs (all -1) has been written.

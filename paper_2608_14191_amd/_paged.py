@@ -137,6 +137,8 @@ def _tokens(func: str, name: str, t, n_tok: int, stride: int, heads: int):
     need = (n_tok - 1) * stride + heads * HEAD_DIM
     if n_tok <= 0 or (t.is_contiguous() and t.numel() >= need):
         return
+    if t.stride(-1) != 1 or (t.dim() > 2 and t.shape[-2] > 1 and t.stride(-2) != HEAD_DIM):
+        _refuse(func, f"the heads and channels of {name} must be contiguous")
     have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
     if have < need:
         _refuse(func, f"{name} holds {have} elements from its first on, {need} are used")
@@ -217,6 +219,8 @@ def aatc_rope(x, n_tok: int, n_heads: int, x_tok_stride: int, pos, rope: Rope, o
     _list(f, "pos", pos, n_tok)
     _tokens(f, "x", x, n_tok, x_tok_stride, n_heads)
     _tokens(f, "out", out, n_tok, out_tok_stride, n_heads)
+    if n_tok == 0:
+        return
     status = entry_point(f)(x.data_ptr(), _dtype(x), n_tok, n_heads, HEAD_DIM, x_tok_stride,
                             pos.data_ptr(), rope.address, 1 if inverse else 0, out.data_ptr(),
                             out_tok_stride, _raw_stream(device) if stream is None else int(stream))
@@ -246,6 +250,8 @@ def aatc_paged_append(cache: PagedCache, table, n_tok: int, k, v, k_tok_stride: 
         _tokens(f, "q", q, n_tok, q_tok_stride, n_q_heads)
         _tokens(f, "q_out", q_out, n_tok, q_out_tok_stride, n_q_heads)
     t, _ = _table(f, table, device)
+    if n_tok == 0:
+        return
     status = entry_point(f)(cache.address, t, n_tok, _dtype(k), k.data_ptr(), k_tok_stride,
                             v.data_ptr(), v_tok_stride, _ptr(seq), pos.data_ptr(),
                             None if rope is None else rope.address, n_q_heads, _ptr(q),

@@ -20,7 +20,7 @@ struct TurnArgs {
   int heads[3];
   void* q_out;
   int64_t q_out_stride;
-  int64_t n_tok;
+  int64_t tok0, n_tok;            // tokens tok0 .. n_tok - 1
   const int32_t* seq;             // sequence of each token, or null: the token's own index
   const int32_t* pos;
   bool skip_negative;             // tokens of negative position are left out (append)

@@ -14,7 +14,8 @@ using namespace aatc;
 namespace {
 
 constexpr int64_t kMaxPages = INT32_MAX;
-constexpr int64_t kMaxList = (int64_t)1 << 30;        // tokens, pairs or rows of one call
+constexpr int64_t kMaxList = (int64_t)1 << 30;        // tokens or pairs of one call
+constexpr int64_t kMaxRows = ((int64_t)1 << 24) - 1;  // rows listed: a workgroup of 256 each
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool known(aatc_dtype t) { return t == AATC_F32 || t == AATC_BF16 || t == AATC_F16; }
@@ -265,7 +266,7 @@ extern "C" aatc_status aatc_paged_decode_attention(
         !tokens_ok(q, q_dtype, q_stride, n_q_heads))
       return AATC_E_INVALID;
     if (!std::isfinite(softmax_scale) || window < 0 || sink < 0 || !(softcap >= 0.f) ||
-        !std::isfinite(softcap))
+        !std::isfinite(softcap) || (softcap > 0.f && !std::isfinite(softmax_scale / softcap)))
       return AATC_E_INVALID;
     if (!out || !aligned(out, 16) || !aligned(lse, 4) || !aligned(slopes, 4) || !workspace ||
         !aligned(workspace, 256))
@@ -342,6 +343,7 @@ extern "C" aatc_status aatc_pages_fork(const aatc_page_table* src, const aatc_pa
     if (src->max_pages != dst->max_pages || n < 0 || n > kMaxList || !pairs || !aligned(pairs, 4))
       return AATC_E_INVALID;
     if (n == 0) return AATC_OK;
+    if (n > kMaxRows) return AATC_E_UNSUPPORTED;
     return launch_pages_fork(*src, *dst, ref, n_pages, pairs, n, stream);
   } catch (...) {
     return AATC_E_INVALID;
@@ -357,6 +359,7 @@ extern "C" aatc_status aatc_pages_free(const aatc_page_table* table, int32_t* re
     if (e != AATC_OK) return e;
     if (n < 0 || n > kMaxList || !rows || !aligned(rows, 4)) return AATC_E_INVALID;
     if (n == 0) return AATC_OK;
+    if (n > kMaxRows) return AATC_E_UNSUPPORTED;
     return launch_pages_free(*table, ref, n_pages, rows, n, stream);
   } catch (...) {
     return AATC_E_INVALID;

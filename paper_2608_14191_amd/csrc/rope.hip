@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
   using CT = typename C::type;
   __shared__ float2 cs[kTurnWaves][kD / 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t tok = (int64_t)blockIdx.x * kTurnWaves + wave;
+  const int64_t tok = a.tok0 + (int64_t)blockIdx.x * kTurnWaves + wave;
   const bool in = tok < a.n_tok;
   const int p = in ? a.pos[tok] : 0;
   const bool on = in && !(a.skip_negative && p < 0);
@@ -223,9 +223,17 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
 }
 
 template <int XD, int CD>
-aatc_status launch_turn_types(const TurnArgs& a, int layout, bool vec, hipStream_t st) {
+aatc_status launch_turn_types(TurnArgs a, int layout, bool vec, hipStream_t st) {
+  // (A launch has less than 2^32 threads.)
+  constexpr int64_t kMost = (int64_t)1 << 25;
+  for (; a.n_tok - a.tok0 > kMost; a.tok0 += kMost) {
+    TurnArgs piece = a;
+    piece.n_tok = a.tok0 + kMost;
+    const aatc_status e = launch_turn_types<XD, CD>(piece, layout, vec, st);
+    if (e != AATC_OK) return e;
+  }
   const int all = a.heads[0] + a.heads[1] + a.heads[2];
-  const int64_t blocks = (a.n_tok + kTurnWaves - 1) / kTurnWaves;
+  const int64_t blocks = (a.n_tok - a.tok0 + kTurnWaves - 1) / kTurnWaves;
   // A wave takes up to 32 heads of its token; with few tokens fewer, so that the chip's compute
   // units all have some.
   int per = all < 32 ? all : 32;

@@ -187,3 +187,99 @@ def test_non_finite_queries_and_values():
     assert torch.all(torch.isfinite(got[0, [0, 2, 3]]))
     assert not torch.any(torch.isfinite(got[1, :2, 7]))
     assert torch.all(torch.isfinite(got[1, :2, :7])) and torch.all(torch.isfinite(got[1, 2:]))
+
+
+@pytest.mark.parametrize("cache,qtype", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32"),
+                                         ("f16", "bf16")])
+def test_queries_of_any_alignment(cache, qtype):
+    """Sequences an odd number of elements apart, the first behind an odd offset."""
+    k, v, table, lens, q = _case(30, [100, 3, 260], 4, 2, 16, cache, qtype)
+    want, _ = _run(k, v, table, lens, q)
+    stride = 4 * D + 3
+    flat = torch.zeros(1 + 3 * stride, dtype=q.dtype)
+    flat[1:].reshape(3, stride)[:, :4 * D] = q.reshape(3, -1)
+    out = torch.empty(3, 4, D, device="cuda")
+    ws = torch.zeros(P.aatc_paged_decode_workspace_bytes(3, 4, 2), dtype=torch.uint8, device="cuda")
+    P.aatc_paged_decode_attention(P.PagedCache(to_cuda(k), to_cuda(v)), table.cuda(), lens.cuda(), 3, 4,
+                                  flat.cuda()[1:], D ** -0.5, out, ws, q_stride=stride)
+    assert torch.equal(out.cpu(), want)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: the results of one after the other."""
+    cases = [_case(31, [3000, 5], 8, 2, 16), _case(32, [50, 900] * 40, 8, 4, 16)]
+    want = [_run(*c)[0] for c in cases]
+    held, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k, v, table, lens, q in cases:
+        ws = torch.zeros(P.aatc_paged_decode_workspace_bytes(len(lens), q.shape[1], k.shape[1]),
+                         dtype=torch.uint8, device="cuda")
+        held.append((P.PagedCache(to_cuda(k), to_cuda(v)), table.cuda(), lens.cuda(), q.cuda(),
+                     torch.zeros(*q.shape, device="cuda"), ws))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (cache, table, lens, q, out, ws), stream in zip(held, streams):
+            P.aatc_paged_decode_attention(cache, table, lens, len(lens), q.shape[1], q, D ** -0.5, out,
+                                          ws, stream=stream.cuda_stream)
+    torch.cuda.synchronize()
+    for (*_, out, _), w in zip(held, want):
+        assert torch.equal(out.cpu(), w)
+
+
+@pytest.mark.parametrize("order", ["head", "token"])
+def test_pools_past_32_bit_offsets(order):
+    """Pages at the end of pools of 2^31 elements and more: append, attention and copy reach them."""
+    hkv, page, n = 8, 64, 150
+    n_pages = (1 << 31) // (hkv * page * D) + 5
+    shape = (n_pages, hkv, page, D) if order == "head" else (n_pages, page, hkv, D)
+    both = torch.zeros((2, *shape), dtype=torch.bfloat16, device="cuda")
+    pools = [x if order == "head" else x.transpose(1, 2) for x in both]
+    cache = P.PagedCache(*pools)
+    table = torch.tensor([[n_pages - 1, 3, n_pages - 3]], dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(n, 2 * hkv, D, generator=g).to(torch.bfloat16)
+    dev = x.cuda()
+    P.aatc_paged_append(cache, table, n, dev[:, :hkv], dev[:, hkv:], 2 * hkv * D, 2 * hkv * D,
+                        torch.zeros(n, dtype=torch.int32, device="cuda"),
+                        torch.arange(n, dtype=torch.int32, device="cuda"))
+    P.aatc_pages_copy(both, torch.tensor([[n_pages - 1, n_pages - 2]], dtype=torch.int32, device="cuda"))
+    table[0, 0] = n_pages - 2
+    both[:, n_pages - 1] = NAN
+    q = torch.randn(1, hkv, D, generator=g)
+    out = torch.empty(1, hkv, D, device="cuda")
+    ws = torch.zeros(P.aatc_paged_decode_workspace_bytes(1, hkv, hkv), dtype=torch.uint8, device="cuda")
+    P.aatc_paged_decode_attention(cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), 1,
+                                  hkv, q.cuda(), D ** -0.5, out, ws)
+    got = out.cpu().double()
+    for h in range(hkv):
+        k, v = x[:, h].double(), x[:, hkv + h].double()
+        want = torch.softmax(k @ q[0, h].double() * D ** -0.5, 0) @ v
+        assert (got[0, h] - want).norm() <= 2e-6 * want.norm()
+
+
+def test_what_the_binding_refuses():
+    """(A slice of a longer tensor of queries is not refused: what is read lies in its storage.)"""
+    k, v, table, lens, q = _case(33, [20, 30], 4, 2, 16)
+    cache = P.PagedCache(k.cuda(), v.cuda())
+    ws = torch.zeros(P.aatc_paged_decode_workspace_bytes(2, 4, 2), dtype=torch.uint8, device="cuda")
+    good = dict(cache=cache, table=table.cuda(), seq_len=lens.cuda(), batch=2, n_q_heads=4, q=q.cuda(),
+                softmax_scale=0.1, out=torch.empty(2, 4, D, device="cuda"), workspace=ws)
+    P.aatc_paged_decode_attention(**good)
+    bad = [dict(q=q), dict(table=table), dict(seq_len=lens), dict(out=torch.empty(2, 4, D)),
+           dict(out=torch.empty(1, 4, D, device="cuda")), dict(out=good["out"].bfloat16()),
+           dict(seq_len=lens.cuda().long()), dict(seq_len=lens.cuda()[:1]), dict(q=q[:1].cuda()),
+           dict(table=table.cuda().long()), dict(table=table.cuda().T), dict(batch=3),
+           dict(workspace=ws[:256]), dict(workspace=ws.cpu()), dict(slopes=torch.ones(3, device="cuda")),
+           dict(lse=torch.ones(7, device="cuda")), dict(q=q.cuda().transpose(1, 2).contiguous().transpose(1, 2))]
+    for change in bad:
+        with pytest.raises(P.AatcError):
+            P.aatc_paged_decode_attention(**{**good, **change})
+    with pytest.raises(TypeError):
+        P.aatc_paged_decode_attention(**{**good, "q": q.cuda().double()})
+    for a, b in ((k.cuda(), v), (k, v)):
+        with pytest.raises(P.AatcError):
+            P.PagedCache(a, b)
+    for a, b in ((k.cuda(), v.cuda()[:3]), (k.cuda(), v.cuda().float()), (k.cuda()[0], v.cuda()[0]),
+                 (k.cuda().transpose(2, 3).contiguous().transpose(2, 3), v.cuda())):
+        with pytest.raises(ValueError):
+            P.PagedCache(a, b)
+    torch.cuda.synchronize()

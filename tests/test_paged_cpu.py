@@ -136,6 +136,7 @@ def test_attention_refusals():
         (INVALID, dict(q=None)), (INVALID, dict(qd=7)), (INVALID, dict(qs=4095)), (INVALID, dict(q=ODD)),
         (INVALID, dict(scale=nan)), (INVALID, dict(window=-1)), (INVALID, dict(sink=-1)),
         (INVALID, dict(cap=-1.0)), (INVALID, dict(cap=nan)), (INVALID, dict(cap=float("inf"))),
+        (INVALID, dict(cap=1e-40)),
         (INVALID, dict(out=None)), (INVALID, dict(out=A + 4)), (INVALID, dict(lse=A + 1)),
         (INVALID, dict(slopes=A + 3)), (INVALID, dict(ws=None)), (INVALID, dict(ws=A + 16))])
     # more tiles than the plan counts: 4 rows of 8 KV heads and 2^24 pages of 128 tokens (2^31
@@ -173,11 +174,11 @@ def test_page_table_refusals():
     _structs("aatc_pages_fork", fork)
     _each("aatc_pages_fork", fork, counts + [
         (INVALID, dict(pairs=None)), (INVALID, dict(pairs=A + 2)), (INVALID, dict(n=-1)), (INVALID, dict(n=1 << 31)),
-        (INVALID, dict(dst=(P.PageTable, {**TABLE, "max_pages": 31})))])
+        (UNSUPPORTED, dict(n=1 << 24)), (INVALID, dict(dst=(P.PageTable, {**TABLE, "max_pages": 31})))])
     free = dict(table=(P.PageTable, TABLE), ref=A, n_pages=100, rows=A, n=0, stream=None)
     assert _call("aatc_pages_free", free) == 0
     _structs("aatc_pages_free", free)
-    _each("aatc_pages_free", free, counts + [(INVALID, dict(rows=None)), (INVALID, dict(n=-1))])
+    _each("aatc_pages_free", free, counts + [(INVALID, dict(rows=None)), (INVALID, dict(n=-1)), (UNSUPPORTED, dict(n=1 << 24))])
     need = P.aatc_pages_workspace_bytes(4, 100)
     reserve = dict(table=(P.PageTable, TABLE), ref=A, n_pages=100, page=16, held=A, wanted=A, pairs=A,
                    lacking=A, ws=A, ws_bytes=1 << 40, stream=None)
