@@ -71,8 +71,8 @@ aatc_status aatc_rope_frequencies(int32_t rot_dim, double base, aatc_rope_scalin
  * out      device, like x with out_tok_stride; may be x itself with the same stride (no other
  *          overlap).
  * n_tok == 0 is a no-op.  Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128).
- * Speed: 16-byte aligned rows, and for HALF a rot_dim / 2 that is a multiple of 16 bytes, are
- * moved in 16-byte pieces; others channel by channel, with the same results.
+ * Speed: 16-byte aligned rows are moved in 16-byte pieces (fastest for INTERLEAVED, and for HALF
+ * with a rot_dim / 2 that fills such pieces); others channel by channel, with the same results.
  */
 aatc_status aatc_rope(const void* x, aatc_dtype dtype, int64_t n_tok, int32_t n_heads, int32_t d,
                       int64_t x_tok_stride, const int32_t* pos, const aatc_rope_spec* spec,

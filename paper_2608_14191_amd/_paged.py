@@ -137,7 +137,12 @@ def _tokens(func: str, name: str, t, n_tok: int, stride: int, heads: int):
     need = (n_tok - 1) * stride + heads * HEAD_DIM
     if n_tok <= 0 or (t.is_contiguous() and t.numel() >= need):
         return
-    if t.stride(-1) != 1 or (t.dim() > 2 and t.shape[-2] > 1 and t.stride(-2) != HEAD_DIM):
+    strides = t.stride()
+    if strides == (stride, HEAD_DIM, 1):               # a view [tokens][heads][128]
+        shape = t.shape
+        if shape[0] >= n_tok and shape[1] >= heads and shape[2] == HEAD_DIM:
+            return
+    if strides[-1] != 1 or (len(strides) > 2 and t.shape[-2] > 1 and strides[-2] != HEAD_DIM):
         _refuse(func, f"the heads and channels of {name} must be contiguous")
     have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
     if have < need:

@@ -69,15 +69,29 @@ __device__ inline C get_chunk(const void* p) {
     return *static_cast<const C*>(p);
 }
 
-// XT: type of the tokens and of q_out, CT: of the pages; INTER: interleaved pairs; VEC: 16-byte
-// aligned rows, and half a multiple of a chunk's elements unless interleaved.
-template <int XD, int CD, bool INTER, bool VEC, bool FAR>
+// LDS written by other lanes of the wave: its accesses are in order, the compiler keeps them so.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// How a head's row is moved.  Whole: in 16-byte chunks, with a lane's partners in a chunk of its own
+// (rows 16-byte aligned, and half a multiple of a chunk's elements unless pairs are interleaved).
+// Shuffled: in chunks, the partners by way of LDS (half of any size: 32534 tokens of eight bf16
+// heads, 2 channels rotated, 75.3 us channel by channel, 38.5 so).  Single: channel by channel
+// (rows of any alignment).
+enum Path { kWhole, kShuffled, kSingle };
+
+// XD: type of the tokens and of q_out, CD: of the pages; INTER: interleaved pairs.
+template <int XD, int CD, bool INTER, Path PATH, bool FAR>
 __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int heads_per_wave) {
   using X = Elem<XD>;
   using C = Elem<CD>;
   using XT = typename X::type;
   using CT = typename C::type;
   __shared__ float2 cs[kTurnWaves][kD / 2];
+  __shared__ __align__(16) XT mix[kTurnWaves][PATH == kShuffled ? 64 * 16 / sizeof(XT) : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t tok = a.tok0 + (int64_t)blockIdx.x * kTurnWaves + wave;
   const bool in = tok < a.n_tok;
@@ -116,8 +130,8 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
     const int hh = h - (h < turned ? a.heads[0] : turned);
     return static_cast<CT*>(h < turned ? a.k_pages : a.v_pages) + slot + hh * a.head_stride;
   };
-  if constexpr (VEC) {
-    constexpr int E = 16 / sizeof(XT);                 // elements of a chunk
+  constexpr int E = 16 / sizeof(XT);                   // elements of a chunk
+  if constexpr (PATH == kWhole) {
     using XC = Chunk<XT, E>;
     using CC = Chunk<CT, E>;
     // Lanes of a head: two chunks each, E apart in the head by 128 / 2, or by `half` for the
@@ -196,6 +210,44 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
         for (int c = rot + E * sub; c < kD; c += E * LH) pass(c);
       }
     }
+  } else if constexpr (PATH == kShuffled) {
+    using XC = Chunk<XT, E>;
+    using CC = Chunk<CT, E>;
+    constexpr int LH = kD / E, HW = 64 / LH;           // lanes per head, heads at a time
+    const int c = E * (lane % LH);
+    XT* row = mix[wave] + lane / LH * kD;
+    for (int h = blockIdx.y * heads_per_wave + lane / LH; h < h_end; h += HW) {
+      const bool to_q = h < a.heads[0], turn = h < turned;
+      if (!to_q && slot < 0) continue;
+      const XC x = get_chunk<FAR, XC>(source(h) + c);
+      if (turn) *reinterpret_cast<XC*>(row + c) = x;
+      wave_sync();
+      float y[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        y[e] = X::get(x.e[e]);
+        const int i = c + e;
+        if (turn && i < rot) {
+          const bool low = i < half;
+          const float2 w = cs[wave][low ? i : i - half];
+          const float other = X::get(row[low ? i + half : i - half]);
+          y[e] = low ? y[e] * w.x - other * w.y : y[e] * w.x + other * w.y;
+        }
+      }
+      wave_sync();
+      if (to_q) {
+        XC o = x;                                      // (channels behind rot keep their bits)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (c + e < rot) o.e[e] = X::put(y[e]);
+        if (c < rot || a.copy_rest) put_chunk<FAR>(q_dest(h) + c, o);
+      } else {
+        CC o;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o.e[e] = C::put(y[e]);
+        put_chunk<FAR>(page_dest(h) + c, o);
+      }
+    }
   } else {
     for (int h = blockIdx.y * heads_per_wave; h < h_end; ++h) {
       const bool to_q = h < a.heads[0], turn = h < turned;
@@ -223,13 +275,13 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
 }
 
 template <int XD, int CD>
-aatc_status launch_turn_types(TurnArgs a, int layout, bool vec, hipStream_t st) {
+aatc_status launch_turn_types(TurnArgs a, int layout, Path path, hipStream_t st) {
   // (A launch has less than 2^32 threads.)
   constexpr int64_t kMost = (int64_t)1 << 25;
   for (; a.n_tok - a.tok0 > kMost; a.tok0 += kMost) {
     TurnArgs piece = a;
     piece.n_tok = a.tok0 + kMost;
-    const aatc_status e = launch_turn_types<XD, CD>(piece, layout, vec, st);
+    const aatc_status e = launch_turn_types<XD, CD>(piece, layout, path, st);
     if (e != AATC_OK) return e;
   }
   const int all = a.heads[0] + a.heads[1] + a.heads[2];
@@ -244,24 +296,26 @@ aatc_status launch_turn_types(TurnArgs a, int layout, bool vec, hipStream_t st) 
     hipLaunchKernelGGL(kernel, grid, dim3(kTurnThreads), 0, st, a, per);
   };
   const bool far = a.n_tok * all * kD * (int64_t)sizeof(typename Elem<XD>::type) > kFarBytes;
-  if (!vec)
-    inter ? launch(turn_kernel<XD, CD, true, false, false>)
-          : launch(turn_kernel<XD, CD, false, false, false>);
+  if (path == kSingle)
+    inter ? launch(turn_kernel<XD, CD, true, kSingle, false>)
+          : launch(turn_kernel<XD, CD, false, kSingle, false>);
+  else if (path == kShuffled)
+    launch(turn_kernel<XD, CD, false, kShuffled, false>);
   else if (far)
-    inter ? launch(turn_kernel<XD, CD, true, true, true>)
-          : launch(turn_kernel<XD, CD, false, true, true>);
+    inter ? launch(turn_kernel<XD, CD, true, kWhole, true>)
+          : launch(turn_kernel<XD, CD, false, kWhole, true>);
   else
-    inter ? launch(turn_kernel<XD, CD, true, true, false>)
-          : launch(turn_kernel<XD, CD, false, true, false>);
+    inter ? launch(turn_kernel<XD, CD, true, kWhole, false>)
+          : launch(turn_kernel<XD, CD, false, kWhole, false>);
   return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
 }
 
 template <int XD>
-aatc_status launch_turn_x(const TurnArgs& a, aatc_dtype c, int layout, bool vec, hipStream_t st) {
+aatc_status launch_turn_x(const TurnArgs& a, aatc_dtype c, int layout, Path path, hipStream_t st) {
   switch (c) {
-    case AATC_F32: return launch_turn_types<XD, AATC_F32>(a, layout, vec, st);
-    case AATC_BF16: return launch_turn_types<XD, AATC_BF16>(a, layout, vec, st);
-    default: return launch_turn_types<XD, AATC_F16>(a, layout, vec, st);
+    case AATC_F32: return launch_turn_types<XD, AATC_F32>(a, layout, path, st);
+    case AATC_BF16: return launch_turn_types<XD, AATC_BF16>(a, layout, path, st);
+    default: return launch_turn_types<XD, AATC_F16>(a, layout, path, st);
   }
 }
 
@@ -270,17 +324,19 @@ aatc_status launch_turn_x(const TurnArgs& a, aatc_dtype c, int layout, bool vec,
 aatc_status launch_turn(const TurnArgs& a, aatc_dtype x_dtype, aatc_dtype c_dtype, int layout,
                         void* stream) {
   const int size = x_dtype == AATC_F32 ? 4 : 2, e = 16 / size;
-  bool vec = layout == AATC_ROPE_INTERLEAVED || a.half % e == 0;
+  bool even = true;                                    // rows of 16-byte chunks
   for (int i = 0; i < 3; ++i)
     if (a.heads[i] > 0)
-      vec = vec && reinterpret_cast<uintptr_t>(a.x[i]) % 16 == 0 && a.x_stride[i] % e == 0;
+      even = even && reinterpret_cast<uintptr_t>(a.x[i]) % 16 == 0 && a.x_stride[i] % e == 0;
   if (a.heads[0] > 0)
-    vec = vec && reinterpret_cast<uintptr_t>(a.q_out) % 16 == 0 && a.q_out_stride % e == 0;
+    even = even && reinterpret_cast<uintptr_t>(a.q_out) % 16 == 0 && a.q_out_stride % e == 0;
+  const bool pairs = layout == AATC_ROPE_INTERLEAVED || a.half % e == 0;
+  const Path path = !even ? kSingle : pairs ? kWhole : kShuffled;
   const hipStream_t st = (hipStream_t)stream;
   switch (x_dtype) {
-    case AATC_F32: return launch_turn_x<AATC_F32>(a, c_dtype, layout, vec, st);
-    case AATC_BF16: return launch_turn_x<AATC_BF16>(a, c_dtype, layout, vec, st);
-    default: return launch_turn_x<AATC_F16>(a, c_dtype, layout, vec, st);
+    case AATC_F32: return launch_turn_x<AATC_F32>(a, c_dtype, layout, path, st);
+    case AATC_BF16: return launch_turn_x<AATC_BF16>(a, c_dtype, layout, path, st);
+    default: return launch_turn_x<AATC_F16>(a, c_dtype, layout, path, st);
   }
 }
 
