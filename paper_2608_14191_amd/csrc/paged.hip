@@ -16,9 +16,9 @@
 // taken 14 lower, so that small weights stay off f16's denormals); queries of another type than
 // the cache's into three.
 //
-// The tiles of all rows (sequence, KV head, 16 query heads) lie in one line that the workgroups
-// share evenly, whatever the lengths.  A row that several workgroups share is joined by the last
-// of them to arrive, in the order of the parts.
+// A row is a sequence, a KV head and up to 16 of its query heads.  How the rows are shared out
+// (paged_plan.h) follows from the lengths, which only the device knows.  A row that several
+// workgroups or waves share is joined by the last of them to arrive, in the order of the parts.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -52,8 +52,6 @@ constexpr int kCoherent = 16;                     // cache policy sc1: device-co
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // Lane l with lane l ^ 16, l ^ 32.
 __device__ inline float over_groups_max(float v) {
