@@ -57,7 +57,7 @@ struct PagedArgs {
   const float* slopes;            // [n_q_heads] or null
   unsigned* counters;
   Partial* parts;
-  int slot_heads;                 // partials of a part slot
+  int parts_bytes, slot_heads;    // of `parts`; partials of a slot
   int batch, n_q_heads, n_kv_heads, G, hg, q_dtype;
   int n_pages, max_pages, page_shift, len_max;    // len_max: tokens that a row can name
   int window, sink;

@@ -41,11 +41,12 @@ constexpr int kLineWaves = 4, kLineGroups = 512;
 constexpr int kMaxRunRows = 256;                  // a workgroup each at least
 constexpr int kPagedHeads = 16;                   // query heads of a row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// The workspace: part slots, two a wave of the lines, then the counters.  (The slots' size is fixed
-// so that the counters, which every call leaves at zero, are in one place for calls of any shape.)
-constexpr int kPartsBytes = 2 * kLineGroups * kLineWaves * kPagedHeads * (int)sizeof(Partial);
-constexpr int kRowStride = 64;                    // counters 256 bytes apart (their atomics
-                                                  // would queue on one cache line)
+// The workspace: arrival counters, one for each worker (a shared row's is its first worker's: no
+// worker has more than one row that others go on with), in one place whatever the shape of a call,
+// then part slots of slot_heads partials.  Counters are 256 bytes apart (their atomics would queue
+// on one cache line) and left at zero.
+constexpr int kWorkers = kLineGroups * kLineWaves, kCounterStride = 64;
+constexpr size_t kCountersBytes = (size_t)kWorkers * kCounterStride * sizeof(unsigned);
 constexpr int kRsrcWord3 = 0x00020000;            // raw buffer descriptor word 3 (gfx950)
 constexpr int kCoherent = 16;                     // cache policy sc1: device-coherent access
 
@@ -299,11 +300,11 @@ struct Full32 {
   }
 };
 
-// tanh to a few ulps: for small |x| the first terms of its odd series (the next is below 2^-25 of
-// x at 0.55), else from exp(-2 |x|).
+// tanh to a few ulps: for small |x| the first terms of its odd series (the next is 4e-8 of x at
+// 0.55), else from exp(-2 |x|).
 __device__ inline float tanh_of(float x) {
   const float y = fabsf(x), s = y * y;
-  float r = 0.0014558343f;                         // 21844 / 6081075, -1382 / 155925, ...
+  float r = 0.0014558343f;                         // 929569 / 638512875, 21844 / 6081075, ...
   r = fmaf(-r, s, 0.003592128f);
   r = fmaf(-r, s, 0.0088632356f);
   r = fmaf(-r, s, 0.021869488f);
@@ -666,7 +667,7 @@ __device__ __forceinline__ void line_of_waves(const PagedArgs& a, LineWay way, i
                                                part_at(me - share.first, n), 0, kCoherent);
     }
     if (parts > 1) {
-      unsigned* counter = a.counters + ((int64_t)seq * rows + row) * kRowStride;
+      unsigned* counter = a.counters + share.first * kCounterStride;
       __builtin_amdgcn_s_waitcnt(0);               // the wave's stores are done
       unsigned before_me = 0u;
       if (lane == 0)
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
   const int block = (int)blockIdx.x, grid = (int)gridDim.x;
   const int rows = a.n_kv_heads * a.hg;            // of a sequence
   // Part slots, Partial [slot_heads] each, stored and loaded where every compute unit sees them.
-  const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, kPartsBytes, kRsrcWord3);
+  const auto slots = __builtin_amdgcn_make_buffer_rsrc(a.parts, (short)0, a.parts_bytes, kRsrcWord3);
 
   auto length = [&](int b) { return min(max(a.seq_len[b], 0), a.len_max); };
   auto tiles_of = [&](int b) { return row_tiles(length(b), a.window, a.sink, TT); };
@@ -936,7 +937,7 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
       }
     }
     if (parts > 1) {
-      unsigned* counter = a.counters + ((int64_t)seq * rows + row) * kRowStride;
+      unsigned* counter = a.counters + (block - part) * kCounterStride;
       __builtin_amdgcn_s_waitcnt(0);               // this thread's stores are done
       __syncthreads();
       if (tid == 0)
@@ -963,20 +964,22 @@ __global__ __launch_bounds__(64 * (RUNS ? kRunWaves : kLineWaves), 2) void paged
   }
 }
 
-size_t counters_bytes(int batch, int n_q_heads, int n_kv_heads) {
-  const int hg = (n_q_heads / n_kv_heads + kPagedHeads - 1) / kPagedHeads;
-  return round256((size_t)batch * n_kv_heads * hg * kRowStride * sizeof(unsigned));
+// Part slots of a call of `rows` rows: a workgroup of the runs has one, a worker of the lines two.
+size_t parts_bytes(int64_t rows, int slot_heads) {
+  const int slots = rows <= kRunGroups / 2 ? kRunGroups : 2 * kWorkers;
+  return (size_t)slots * slot_heads * sizeof(Partial);
 }
 
 }  // namespace
 
 size_t paged_workspace_bytes(int batch, int n_q_heads, int n_kv_heads) {
-  return kPartsBytes + counters_bytes(batch, n_q_heads, n_kv_heads);
+  const int G = n_q_heads / n_kv_heads, hg = (G + kPagedHeads - 1) / kPagedHeads;
+  return kCountersBytes + parts_bytes((int64_t)batch * n_kv_heads * hg, std::min(G, kPagedHeads));
 }
 
 aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
-  a.parts = static_cast<Partial*>(workspace);
-  a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kPartsBytes);
+  a.counters = static_cast<unsigned*>(workspace);
+  a.parts = reinterpret_cast<Partial*>(static_cast<char*>(workspace) + kCountersBytes);
   const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
@@ -985,6 +988,7 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   // to 12000 tokens 201.7, as lines 161.8).
   const bool runs = rows <= kRunGroups / 2 || (rows <= kMaxRunRows && a.len_max <= 128 * tt);
   a.slot_heads = std::min(a.G, kPagedHeads);
+  a.parts_bytes = (int)parts_bytes(rows, a.slot_heads);
   const int grid = (int)std::min<int64_t>(runs ? kRunGroups : kLineGroups, most);
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](auto kernel) {
