@@ -297,3 +297,36 @@ def test_fork_write_compact_and_compress():
     P.aatc_encode(pk, hkv, torch.stack(tokens[1][0][:page]).cuda(), page, hkv * D, P.LAYOUT_RECORDS,
                   again, beta, 64, 0)
     assert torch.equal(codes, again) and torch.equal(alpha, beta)
+
+
+def test_joined_attention_in_a_graph():
+    """Captured once, replayed with other lengths and queries, with eager calls between."""
+    B, H, hq, page = 2, 8, 16, 32
+    pk, pv, kc, ka, vc, va, rk, rv, cap, _, _ = _compressed(B, H, [200, 333])
+    g = torch.Generator().manual_seed(9)
+    kp, vp = (pool(g, 40, H, page, torch.bfloat16).cuda() for _ in range(2))
+    cache = P.PagedCache(kp, vp)
+    table = torch.randperm(40, generator=g).reshape(2, 20).int().cuda()
+    n, m = torch.tensor([200, 333]).int().cuda(), torch.tensor([600, 7]).int().cuda()
+    q = torch.randn(B, hq, D, generator=g).cuda()
+    spaces = [torch.zeros(P.aatc_decode_paged_workspace_bytes(B, hq, H, cap), dtype=torch.uint8, device="cuda")
+              for _ in range(2)]
+    outs = [torch.zeros(B, hq, D, device="cuda") for _ in range(2)]
+
+    def call(i):
+        P.aatc_decode_attention_paged(pk, pv, B, hq, H, q, kc, ka, vc, va, n, cap, rk, rv, SCALE, cache,
+                                      table, m, outs[i], spaces[i])
+    call(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(0)
+    for lens, pages in (([200, 333], [600, 7]), ([0, 100], [640, 0]), ([1, 64], [0, 129]), ([200, 0], [33, 0])):
+        n.copy_(torch.tensor(lens).int())
+        m.copy_(torch.tensor(pages).int())
+        q.copy_(torch.randn(B, hq, D, generator=g))
+        outs[0].fill_(float("nan"))
+        graph.replay()
+        call(1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and torch.all(torch.isfinite(outs[0]))
