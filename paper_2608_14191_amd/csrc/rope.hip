@@ -42,8 +42,18 @@ template <>
 struct Elem<AATC_F16> {
   using type = _Float16;
   static __device__ float get(_Float16 x) { return (float)x; }
-  static __device__ _Float16 put(float x) { return (_Float16)x; }
+  // (The compiler may not see where x comes from: a product and sum that it rounds to f16 in one
+  // instruction, in some instances of the kernel only, would differ from the float32 sum's rounding.)
+  static __device__ _Float16 put(float x) {
+    asm("" : "+v"(x));
+    return (_Float16)x;
+  }
 };
+
+// The turned pair.  The same operations in every instance of the kernel, so that a token's bits do
+// not depend on its row's alignment or on how many others the call has.
+__device__ inline float turned_low(float a, float b, float2 w) { return fmaf(a, w.x, -(b * w.y)); }
+__device__ inline float turned_high(float a, float b, float2 w) { return fmaf(a, w.y, b * w.x); }
 
 template <class T, int E>
 struct alignas(sizeof(T) * E < 16 ? sizeof(T) * E : 16) Chunk {
@@ -186,8 +196,8 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
             const int i = (c + e) / 2;
             const float2 w = cs[wave][i < half ? i : 0];
             const float u0 = X::get(x.e[e]), u1 = X::get(x.e[e + 1]);
-            y[e] = i < half ? u0 * w.x - u1 * w.y : u0;
-            y[e + 1] = i < half ? u1 * w.x + u0 * w.y : u1;
+            y[e] = i < half ? turned_low(u0, u1, w) : u0;
+            y[e + 1] = i < half ? turned_high(u0, u1, w) : u1;
           }
           store(c, y);
         }
@@ -201,8 +211,8 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
           for (int e = 0; e < E; ++e) {
             const float2 w = cs[wave][c + e];
             const float u0 = X::get(x0.e[e]), u1 = X::get(x1.e[e]);
-            y0[e] = u0 * w.x - u1 * w.y;
-            y1[e] = u1 * w.x + u0 * w.y;
+            y0[e] = turned_low(u0, u1, w);
+            y1[e] = turned_high(u0, u1, w);
           }
           store(c, y0);
           store(half + c, y1);
@@ -231,7 +241,7 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
           const bool low = i < half;
           const float2 w = cs[wave][low ? i : i - half];
           const float other = X::get(row[low ? i + half : i - half]);
-          y[e] = low ? y[e] * w.x - other * w.y : y[e] * w.x + other * w.y;
+          y[e] = low ? turned_low(y[e], other, w) : turned_high(other, y[e], w);
         }
       }
       wave_sync();
@@ -263,8 +273,8 @@ __global__ __launch_bounds__(kTurnThreads) void turn_kernel(TurnArgs a, int head
         const int c0 = INTER ? 2 * lane : lane, c1 = INTER ? 2 * lane + 1 : lane + half;
         const float2 w = cs[wave][lane];
         const float u0 = X::get(src[c0]), u1 = X::get(src[c1]);
-        put(c0, u0 * w.x - u1 * w.y);
-        put(c1, u1 * w.x + u0 * w.y);
+        put(c0, turned_low(u0, u1, w));
+        put(c1, turned_high(u0, u1, w));
       }
       for (int c = (turn ? rot : 0) + lane; c < kD; c += 64) {
         if (!to_q) put(c, X::get(src[c]));
