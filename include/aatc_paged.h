@@ -145,8 +145,11 @@ aatc_status aatc_paged_append(const aatc_paged_cache* cache, const aatc_page_tab
  *   out = sum_t softmax(z)_t v_t,   lse = ln sum_t exp(z_t),
  * over tokens t < seq_len[b] whose page exists and, with a window, t >= seq_len[b] - window or
  * t < sink.  A head without any such token gets zeros and lse -infinity.  What the pages hold
- * elsewhere (infinities and NaN among it) does not matter; an infinity or NaN in an attended key
- * or value, or in a query, gives infinities or NaN in what it enters.
+ * elsewhere (infinities and NaN among it) does not matter.  NaN in an attended key or in a query
+ * gives NaN, an infinity or NaN in an attended value infinities or NaN in its channel.  Infinite
+ * scores follow the formula: +infinity gives NaN, -infinity has no weight, with a cap they are
+ * +-softcap; a head all of whose attended scores are -infinity gets NaN and lse -infinity.  (Where
+ * 16-bit pages meet queries of another type, infinite keys and queries may give NaN instead.)
  * Products are of the stored values, with sums and softmax in 32 bits.  The result does not
  * depend on timing, but in its last bits on how a batch's tokens are split.
  *

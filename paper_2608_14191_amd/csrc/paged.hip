@@ -23,6 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "paged.h"
@@ -41,6 +42,10 @@ constexpr int kLineWaves = 4, kLineGroups = 512;
 constexpr int kMaxRunRows = 256;                  // a workgroup each at least
 constexpr int kPagedHeads = 16;                   // query heads of a row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The maximum of a part that has attended tokens, all with scores of -infinity (a part without
+// attended tokens has -infinity and the sum 0).  Its sum is not 0, so that a head without any finite
+// score ends as the NaN that its softmax is; beside finite scores it has no weight.
+constexpr float kLowest = -FLT_MAX;
 // The workspace: arrival counters, one for each worker (a shared row's is its first worker's: no
 // worker has more than one row that others go on with), in one place whatever the shape of a call,
 // then part slots of slot_heads partials.  Counters are 256 bytes apart (their atomics would queue
@@ -416,6 +421,8 @@ __device__ inline void join_parts(JoinSpace<W, GROUPS>& sh, int parts, int heads
 // What a row ends as: outputs and log-sum-exp, or a partial for another join.  Four channels of a
 // head.
 __device__ inline void finish_row(const PagedArgs& a, int64_t head, int c4, float m, float l, v4f o) {
+  const bool lost = m == kLowest && l == l;        // every attended score was -infinity (none NaN)
+  if (lost) o = (v4f){NAN, NAN, NAN, NAN};
   if (a.seg) {
     Partial* s = a.seg + head;
     reinterpret_cast<v4f*>(s->o)[c4] = o;
@@ -424,7 +431,7 @@ __device__ inline void finish_row(const PagedArgs& a, int64_t head, int c4, floa
   }
   const v4f zero = {0.f, 0.f, 0.f, 0.f};
   reinterpret_cast<v4f*>(a.out)[head * (kD / 4) + c4] = l == 0.f ? zero : o / l;
-  if (a.lse && c4 == 0) a.lse[head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (a.lse && c4 == 0) a.lse[head] = l == 0.f || lost ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // What one wave has of a row: for head n of its lanes the maximum, the sum and the value sums
@@ -525,6 +532,7 @@ struct Walk {
     const int last = s.last, step = s.step;
     int t0 = s.t0, vp = s.vp, t1 = s.t1, kp1 = s.kp1, vp1 = s.vp1;
     float m_run = -INFINITY, l_run = 0.f;
+    bool seen = false;                             // any token attended (of the wave's, uniform)
     v4f(&acc)[8] = out.acc;
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
@@ -553,6 +561,7 @@ struct Walk {
       const bool whole = t0 + TT <= len && (t0 >= lo || t0 + TT <= a.sink) &&
                          __builtin_amdgcn_ballot_w64(!there) == 0;
       if (!whole) {
+        bool any = false;
 #pragma unroll
         for (int e = 0; e < NM; ++e) {
           const int t = t0 + NM * g + e;
@@ -560,7 +569,11 @@ struct Walk {
           const bool on = there & (t < len) & ((t >= lo) | (t < a.sink));
           z[e] = on ? z[e] : -INFINITY;
           val.keep(e, on);
+          any |= on;
         }
+        seen |= __builtin_amdgcn_ballot_w64(any) != 0;
+      } else {
+        seen = true;
       }
       float m = z[0];
 #pragma unroll
@@ -585,6 +598,10 @@ struct Walk {
     }
     out.m = m_run;
     out.l = over_groups_sum(l_run);
+    if (seen && out.m == -INFINITY && out.l == 0.f) {     // (NaN scores: the sum is NaN)
+      out.m = kLowest;
+      out.l = 1.f;
+    }
   }
 };
 
