@@ -205,7 +205,7 @@ aatc_status aatc_decode_attention_paged(
 /*
  * Page tables on the device.  ref[i] counts the table entries that name page i; pages of count 0
  * are free.  Whole numbers only, and always the same result: nothing depends on timing.  Table
- * entries outside [0, n_pages) are skipped.
+ * entries outside [0, n_pages) are skipped; a new table is filled with -1.
  *
  * aatc_pages_fork -- the rows pairs[i][1] of dst become copies of the rows pairs[i][0] of src
  * (the same or another table, of as many entries per row), and their pages' counts go up: beams
@@ -225,12 +225,14 @@ aatc_status aatc_pages_free(const aatc_page_table* table, int32_t* ref, int64_t 
 /*
  * aatc_pages_reserve -- makes room for the tokens held[b] .. wanted[b] - 1 of every row b.
  *
- * Entries of the pages that begin there take free pages, the lowest first, row after row.  Where
- * the first of those tokens falls into a page that is already begun and that other entries name
- * too, the row gets a free page of its own for it: pairs[b] = (old, new), for aatc_pages_copy
- * (of rows of one call that share a page to the last entry, the last one keeps it).  pairs[b] =
- * (-1, -1) elsewhere.  A begun page that is not there gets none.  Lengths are clamped to [0, max_pages * page_tokens]; wanted[b] <= held[b]
- * asks for nothing.
+ * Entries of the pages that these tokens fall into that name no page (or a free one) take free
+ * ones, the lowest first, row after row; a begun page that is not there gets none.  Entries that name a page already
+ * (reserved ahead, left by a rollback) keep it where no other entry names it.  Where others do, the
+ * row gets a free page of its own and the old one's count goes down (of claims of one call on one
+ * page that nobody else holds, the last in the order of rows and entries keeps it).  For the begun
+ * page that the first of the tokens falls into, pairs[b] = (old, new) then, for aatc_pages_copy;
+ * elsewhere pairs[b] = (-1, -1).  Lengths are clamped to [0, max_pages * page_tokens];
+ * wanted[b] <= held[b] asks for nothing.
  * lacking  device [1] int32: 0, or how many free pages there were too few: then nothing but
  *          lacking and pairs (all -1) has been written.
  * held, wanted  device [rows] int32.  pairs  device [rows][2] int32.

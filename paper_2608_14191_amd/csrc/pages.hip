@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -116,18 +117,28 @@ __global__ __launch_bounds__(kListThreads) void free_kernel(int32_t* table, int6
 }
 
 // ---------------------------------------------------------------------------------------
-// Reserve: one workgroup.  For every row the first of its places in the list of free pages to hand
-// out and its partial page to leave (-1: none), and that list, are in LDS as far as they fit (the
-// round trips to memory are the time: 128 children of 32 parents 12.0 us with all of them in the
-// workspace), else in the workspace.
+// Reserve: one workgroup.  A row's claims are the entries that its new tokens fall into, the begun
+// page first where there is one; claims are numbered row after row, entry after entry.  A claim wants
+// a free page where its entry names none (a begun one then gets none), or one that other entries
+// name too, unless all of those are earlier claims that leave it.  Wants get their places in the list
+// of free pages in the order of the claims.
+//
+// The rows' first claims, the wants and the free pages are in LDS as far as they fit (the round trips
+// to memory are the time: 128 children of 32 parents 12.0 us with all of them in the workspace), else
+// in the workspace, which also counts the earlier claims of a page over several steps.  Where no row
+// has two claims (a decode step) claim i is row i's; else they are numbered by a scan and found by a
+// search, four a thread and step where they are many.
 struct ReserveSpace {
-  int32_t *place, *leave, *free;
+  int32_t *first, *row, *entry, *free;
 };
-__host__ __device__ inline ReserveSpace reserve_space(void* ws, int64_t rows) {
+__host__ __device__ inline ReserveSpace reserve_space(void* ws, int64_t rows, int64_t n_pages) {
   auto* p = static_cast<int32_t*>(ws);
-  return {p, p + rows, p + 2 * rows};
+  return {p, p + rows, p + rows + n_pages, p + rows + 2 * n_pages};
 }
-constexpr int kFreeLds = 2048;
+constexpr int kListLds = 2048;
+constexpr int kManyClaims = 4;                  // a thread and step
+constexpr int kBegun = 1 << 30;                 // of a want's entry (below 2^30): the row's begun page,
+constexpr int kShared = (int)(1u << 31);        // a page that others keep
 
 template <int PP>
 __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
@@ -135,30 +146,21 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     const int32_t* __restrict__ held, const int32_t* __restrict__ wanted, int32_t* pairs,
     int32_t* lacking, void* ws) {
   __shared__ int scratch[kPlanWaves];
-  __shared__ int chunk[kPlanThreads], place_s[kPlanThreads], leave_s[kPlanThreads], free_s[kFreeLds];
+  __shared__ int chunk[kPlanThreads * kManyClaims], first_s[kPlanThreads], from_s[kPlanThreads];
+  __shared__ int row_s[kListLds], entry_s[kListLds], free_s[kListLds];
   const int tid = threadIdx.x;
-  const ReserveSpace sp = reserve_space(ws, rows);
+  const ReserveSpace sp = reserve_space(ws, rows, n_pages);
   const bool small = rows <= kPlanThreads;
-  auto place_of = [&](int r) { return small ? place_s[r] : sp.place[r]; };
-  auto leave_of = [&](int r) { return small ? leave_s[r] : sp.leave[r]; };
-  auto free_page = [&](int i) { return i < kFreeLds ? free_s[i] : sp.free[i]; };
   const int mask = (1 << shift) - 1;
-  // Row r: tokens from .. to - 1 to come.
+  // Row r: tokens from .. to - 1 to come, and its claims.
+  auto length = [&](const int32_t* list, int r) { return min(max(list[r], 0), len_max); };
   struct Row {
-    int from, to;
-    __device__ bool grows() const { return to > from; }
+    int from, claims;
   };
   auto row_of = [&](int r) {
-    return Row{min(max(held[r], 0), len_max), min(max(wanted[r], 0), len_max)};
-  };
-  // The begun page that row r's first new token falls into (-1: none).
-  auto partial_of = [&](int r, const Row& w) {
-    if (!w.grows() || !(w.from & mask)) return -1;
-    const int page = table[r * stride + (w.from >> shift)];
-    return page >= 0 && page < n_pages ? page : -1;
-  };
-  auto new_pages = [&](const Row& w) {
-    return w.grows() ? ((w.to + mask) >> shift) - ((w.from + mask) >> shift) : 0;
+    if (r >= rows) return Row{0, 0};
+    const int from = length(held, r), to = length(wanted, r);
+    return Row{from, to > from ? ((to + mask) >> shift) - (from >> shift) : 0};
   };
   // The free ones of this thread's pages of a step, a bit each (the first step's are read now).
   auto open_pages = [&](int64_t base) {
@@ -171,39 +173,124 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     return open;
   };
   const unsigned open0 = open_pages(0);
-  // (1) What each row needs: a page in the place of one that others hold too, unless every other
-  // holder is an earlier row of this call that gets a copy, and its new pages.
-  int demand = 0;
-  for (int base = 0; base < rows; base += kPlanThreads) {
-    const int r = base + tid;
-    const Row w = r < rows ? row_of(r) : Row{0, 0};
-    const int mine = r < rows ? partial_of(r, w) : -1;
-    const int count = mine >= 0 ? ref[mine] : 0;
-    int earlier = 0;
-    if (__syncthreads_or(count > 1)) {
-      for (int b = 0; b <= base; b += kPlanThreads) {
-        const int other = b + tid;
-        const int page = b == base ? mine : partial_of(other, row_of(other));
-        __syncthreads();
-        chunk[tid] = page;
-        __syncthreads();
-        if (count > 1) {
-          const int upto = b == base ? tid : kPlanThreads;
-#pragma unroll 8
-          for (int k = 0; k < upto; ++k) earlier += chunk[k] == mine;
+  // (1) The rows' claims.
+  const Row row0 = row_of(tid);
+  int more = row0.claims > 1;
+  for (int r = tid; r < rows; r += kPlanThreads) {
+    if (r != tid) more |= row_of(r).claims > 1;
+    pairs[2 * r] = -1;
+    pairs[2 * r + 1] = -1;
+  }
+  const bool one = !__syncthreads_or(more);     // claim i is row i's (some have none)
+  int claims = one ? rows : 0;
+  if (!one)
+    for (int base = 0; base < rows; base += kPlanThreads) {
+      const int r = base + tid;
+      const Row w = base == 0 ? row0 : row_of(r);
+      int sum = 0;
+      const int first = claims + block_scan(w.claims, sum, scratch);
+      if (r < rows) {
+        if (small) {
+          first_s[r] = first;
+          from_s[r] = w.from;
+        } else {
+          sp.first[r] = first;
         }
       }
+      claims += sum;
     }
-    const bool copy = count - earlier > 1;
-    int sum = 0;
-    const int place = demand + block_scan((copy ? 1 : 0) + new_pages(w), sum, scratch);
-    if (r < rows) {
-      (small ? place_s : sp.place)[r] = place;
-      (small ? leave_s : sp.leave)[r] = copy ? mine : -1;
+  // (2) What they want.  `earlier`, in the place of the free pages' list: claims of each shared page
+  // in the steps before.
+  int32_t* earlier = sp.free;
+  const bool many = !one && claims > kPlanThreads;
+  const int step = kPlanThreads * (many ? kManyClaims : 1);
+  const bool steps = claims > step;
+  if (steps)
+    for (int64_t p = tid; p < n_pages; p += kPlanThreads)
+      __hip_atomic_store(&earlier[p], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __builtin_amdgcn_s_waitcnt(0);                // (a barrier does not wait for stores)
+  __syncthreads();
+  auto wants_of = [&](auto per, int base, int demand) {
+    constexpr int K = decltype(per)::value;
+    int row[K], entry[K], page[K], count[K];    // (entry: with kBegun, and kShared later)
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = (int)plan_page<K>(base, k);
+      bool on = i < claims;
+      int r, from, at;                          // its `at`th claim
+      if (one) {
+        const Row w = base == 0 ? row0 : row_of(i);
+        r = min(i, rows - 1), from = w.from, at = 0;
+        on = w.claims > 0;
+      } else {
+        const int x = min(i, claims - 1);
+        r = 0;
+        int hi = rows - 1, first = small ? first_s[0] : sp.first[0];
+        while (r < hi) {                        // the last row whose claims begin at or before x
+          const int mid = (r + hi + 1) / 2, f = small ? first_s[mid] : sp.first[mid];
+          if (f <= x) r = mid, first = f;
+          else hi = mid - 1;
+        }
+        from = small ? from_s[r] : length(held, r);
+        at = x - first;
+      }
+      row[k] = r;
+      entry[k] = on ? (from >> shift) + at : 0;
+      page[k] = table[r * stride + entry[k]];
+      page[k] = on && page[k] >= 0 && page[k] < n_pages ? page[k] : -1;
+      entry[k] |= at == 0 && (from & mask) != 0 ? kBegun : 0;
+      row[k] = on ? r : -1;
     }
-    demand += sum;
-  }
-  // (2) The lowest free pages, as many.
+    int shared = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = ref[max(page[k], 0)];
+      count[k] = page[k] >= 0 ? c : 0;
+      shared |= count[k] > 1;
+    }
+    if (__syncthreads_or(shared)) {             // pages that others name too: who leaves them?
+#pragma unroll
+      for (int k = 0; k < K; ++k) chunk[(int)plan_page<K>(0, k)] = count[k] > 1 ? page[k] : -1;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (count[k] <= 1) continue;
+        int before = steps ? __hip_atomic_load(&earlier[page[k]], __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT)
+                           : 0;
+        const int upto = (int)plan_page<K>(0, k);
+#pragma unroll 8
+        for (int j = 0; j < upto; ++j) before += chunk[j] == page[k];
+        if (count[k] - before > 1) entry[k] |= kShared;
+      }
+      __syncthreads();                          // (the counts are read)
+      if (steps) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (count[k] > 1)
+            __hip_atomic_fetch_add(&earlier[page[k]], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_s_waitcnt(0);          // (the barriers below come before the next step)
+      }
+    }
+    return rank_pages<K>(demand, scratch, [&](int k) {
+      return row[k] >= 0 && ((entry[k] & kShared) != 0 || ((entry[k] & kBegun) == 0 && count[k] <= 0));
+    }, [&](int rank, int k) {
+      if (rank >= n_pages) return;              // (more than there can be)
+      if (rank < kListLds) {
+        row_s[rank] = row[k];
+        entry_s[rank] = entry[k];
+      } else {
+        sp.row[rank] = row[k];
+        sp.entry[rank] = entry[k];
+      }
+    });
+  };
+  int demand = 0;
+  for (int base = 0; base < claims; base += step)
+    demand += many ? wants_of(std::integral_constant<int, kManyClaims>{}, base, demand)
+                   : wants_of(std::integral_constant<int, 1>{}, base, demand);
+  __syncthreads();                              // (`earlier` is read: the free pages go there)
+  // (3) The lowest free pages, as many.
   int found = 0;
   for (int64_t base = 0; base < n_pages && found < demand; base += kPlanThreads * PP) {
     const unsigned open = base == 0 ? open0 : open_pages(base);
@@ -211,39 +298,29 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
                         [&](int rank, int k) {
                           if (rank >= demand) return;
                           const int page = (int)plan_page<PP>(base, k);
-                          if (rank < kFreeLds) free_s[rank] = page;
+                          if (rank < kListLds) free_s[rank] = page;
                           else sp.free[rank] = page;
                         });
   }
-  __syncthreads();                              // (the list is this workgroup's own)
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();                              // (the lists are this workgroup's own)
   const bool enough = found >= demand;
   if (tid == 0) *lacking = enough ? 0 : demand - found;
-  // (3) Hand out.
-  for (int r = tid; r < rows; r += kPlanThreads) {
-    const int old = enough ? leave_of(r) : -1;
-    int now = -1;
-    if (old >= 0) {
-      now = free_page(place_of(r));
-      table[r * stride + (row_of(r).from >> shift)] = now;
-      atomicAdd(&ref[old], -1);
-      ref[now] = 1;
-    }
-    pairs[2 * r] = old;
-    pairs[2 * r + 1] = now;
-  }
   if (!enough) return;
+  // (4) Hand out.
   for (int i = tid; i < demand; i += kPlanThreads) {
-    int lo = 0, hi = rows - 1;                  // the last row whose places begin at or before i
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (place_of(mid) <= i) lo = mid;
-      else hi = mid - 1;
+    const bool lds = i < kListLds;
+    const int row = lds ? row_s[i] : sp.row[i], e = lds ? entry_s[i] : sp.entry[i];
+    const int now = lds ? free_s[i] : sp.free[i];
+    int32_t* at = table + row * stride + (e & (kBegun - 1));
+    const int old = e & kShared ? *at : -1;
+    *at = now;
+    ref[now] = 1;
+    if (old >= 0) atomicAdd(&ref[old], -1);
+    if (e & kBegun) {
+      pairs[2 * row] = old;
+      pairs[2 * row + 1] = now;
     }
-    const int k = i - place_of(lo) - (leave_of(lo) >= 0 ? 1 : 0);
-    if (k < 0) continue;                        // the copy's
-    const int page = free_page(i);
-    table[lo * stride + ((row_of(lo).from + mask) >> shift) + k] = page;
-    ref[page] = 1;
   }
 }
 
@@ -393,7 +470,7 @@ aatc_status launch_pages_free(const aatc_page_table& t, int32_t* ref, int64_t n_
 }
 
 size_t pages_workspace_bytes(int64_t rows, int64_t n_pages) {
-  return (size_t)(2 * rows + n_pages) * sizeof(int32_t);
+  return (size_t)(rows + 3 * n_pages) * sizeof(int32_t);       // (ReserveSpace; a compaction: n_pages)
 }
 
 aatc_status launch_pages_reserve(const aatc_page_table& t, int32_t* ref, int64_t n_pages,
