@@ -151,14 +151,16 @@ def _tokens(func: str, name: str, t, n_tok: int, stride: int, heads: int):
 
 def _table(func: str, table, device: int):
     """(aatc_page_table as an argument, rows) of a PageTable or an int32 tensor."""
-    if isinstance(table, PageTable):
+    handle = isinstance(table, PageTable)
+    t = table.tensor if handle else table
+    if t.get_device() != device:
+        _refuse(func, f"the page table is on {t.device}, the current device is cuda:{device}")
+    if handle:
         return ctypes.addressof(table), table.rows
     rows, entries = table.shape
     across, along = table.stride()
     if table.dtype != _TORCH.int32 or (entries > 1 and along != 1):
         _refuse(func, "a page table must be an int32 tensor [rows][max_pages], rows contiguous")
-    if table.get_device() != device:
-        _refuse(func, f"the page table is on {table.device}, the current device is cuda:{device}")
     return _pack_table(table.data_ptr(), across if rows > 1 else entries, rows, entries), rows
 
 

@@ -1,0 +1,97 @@
+"""What the binding of the paged calls checks before it calls the library, without a GPU: tensors that
+claim to be on a device, and the library's entry points replaced by a record of their calls."""
+import pytest
+import torch
+
+import paper_2608_14191_amd as P
+from paper_2608_14191_amd import _paged
+
+
+class _On(torch.Tensor):
+    """A CPU tensor that says it is on GPU `where`."""
+
+    where = 0
+
+    def get_device(self):
+        return self.where
+
+
+def _on(t, where=0):
+    t = t.as_subclass(_On)
+    t.where = where
+    return t
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    _paged._torch()
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(_paged, "_device", lambda: 0)
+    monkeypatch.setattr(_paged, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(_paged, "entry_point", lambda name: lambda *a: made.append(name) or 0)
+    return made
+
+
+def _i32(*shape, where=0):
+    return _on(torch.zeros(*shape, dtype=torch.int32), where)
+
+
+def _cache(pages=4, heads=2, page=16):
+    return P.PagedCache(*(_on(torch.zeros(pages, heads, page, 128)) for _ in range(2)))
+
+
+def _floats(*shape):
+    return _on(torch.zeros(*shape))
+
+
+def _space():
+    return _on(torch.zeros(64, dtype=torch.uint8))
+
+
+def _calls_with(table):
+    """Every call that takes a page table, with `table` in its place."""
+    x, good = _floats(1, 2, 128), _i32(2, 3)
+    return {
+        "aatc_paged_append": lambda: P.aatc_paged_append(_cache(), table, 1, x, x, 256, 256, None, _i32(1)),
+        "aatc_paged_decode_attention": lambda: P.aatc_paged_decode_attention(
+            _cache(), table, _i32(1), 1, 2, x, 0.1, _floats(1, 2, 128), _space()),
+        "aatc_decode_attention_paged": lambda: P.aatc_decode_attention_paged(**{**_joined(), "table": table}),
+        "aatc_pages_fork": lambda: P.aatc_pages_fork(table, good, _i32(4), _i32(1, 2)),
+        "aatc_pages_fork ": lambda: P.aatc_pages_fork(good, table, _i32(4), _i32(1, 2)),
+        "aatc_pages_free": lambda: P.aatc_pages_free(table, _i32(4), _i32(1)),
+        "aatc_pages_reserve": lambda: P.aatc_pages_reserve(table, _i32(4), 16, _i32(2), _i32(2), _i32(2, 2),
+                                                           _i32(1), _space()),
+        "aatc_pages_compact": lambda: P.aatc_pages_compact(table, _i32(4), good, _i32(4), _i32(2, 2), _i32(1),
+                                                           _space()),
+        "aatc_pages_compact ": lambda: P.aatc_pages_compact(good, _i32(4), table, _i32(4), _i32(2, 2), _i32(1),
+                                                            _space()),
+    }
+
+
+def _joined():
+    """Arguments of the joined attention: two sequences, two KV heads, 64 tokens, 44-byte records."""
+    u8 = lambda *s: _on(torch.zeros(*s, dtype=torch.uint8))                      # noqa: E731
+    alpha = lambda: _on(torch.zeros(2, 2, 64, dtype=torch.int16))               # noqa: E731
+    params = P.library().aatc_params_bytes(2)
+    return dict(dev_params_k=u8(params), dev_params_v=u8(params), batch=2, n_q_heads=4, n_kv_heads=2,
+                q=_floats(2, 4, 128), k_codes=u8(2, 2, 64, 44), k_alpha=alpha(), v_codes=u8(2, 2, 1, 64 * 44),
+                v_alpha=alpha(), seq_len=_i32(2), cap=64, k_record_bytes=44, v_record_bytes=44,
+                softmax_scale=0.1, cache=_cache(), table=_i32(2, 3), page_len=_i32(2),
+                out=_floats(2, 4, 128), workspace=_space())
+
+
+@pytest.mark.parametrize("name", sorted(_calls_with(None)))
+def test_page_tables_on_another_device(calls, monkeypatch, name):
+    """As a tensor and as a handle, which may have been made while its device was the current one."""
+    for table in (_i32(2, 3), P.PageTable(_i32(2, 3))):
+        _calls_with(table)[name]()
+    assert calls == [name.strip()] * 2
+    monkeypatch.setattr(_paged, "_device", lambda: 1)
+    handle = P.PageTable(_i32(2, 3, where=1))
+    monkeypatch.setattr(_paged, "_device", lambda: 0)
+    for table in (_i32(2, 3, where=1), handle):
+        with pytest.raises(P.AatcError) as e:
+            _calls_with(table)[name]()
+        assert e.value.status == 1 and "device" in str(e.value)
+    assert len(calls) == 2
