@@ -272,8 +272,10 @@ def aatc_paged_decode_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: in
     return int(entry_point("aatc_paged_decode_workspace_bytes")(batch, n_q_heads, n_kv_heads))
 
 
-def _bytes(workspace) -> int:
-    return workspace.numel() * workspace.element_size()
+def _buffer(func: str, name: str, t, n: int):
+    """A contiguous tensor of any type that holds n bytes."""
+    if not t.is_contiguous() or t.nbytes < n:
+        _refuse(func, f"{name} must be a contiguous tensor of at least {n} bytes")
 
 
 def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n_q_heads: int, q,
@@ -318,7 +320,17 @@ def aatc_decode_attention_paged(dev_params_k, dev_params_v, batch: int, n_q_head
     _list(f, "seq_len", seq_len, batch)
     _list(f, "page_len", page_len, batch)
     _floats(f, "out", out, batch * n_q_heads * HEAD_DIM)
-    _tokens(f, "q", q, batch, n_q_heads * HEAD_DIM, n_q_heads)
+    if not q.is_contiguous() or q.numel() < batch * n_q_heads * HEAD_DIM:
+        _refuse(f, "q must be a contiguous tensor [batch][n_q_heads][128]")
+    params, tokens = _lib.aatc_params_bytes(n_kv_heads), batch * n_kv_heads * cap
+    _buffer(f, "dev_params_k", dev_params_k, params)
+    _buffer(f, "dev_params_v", dev_params_v, params)
+    _buffer(f, "k_codes", k_codes, tokens * k_record_bytes)
+    _buffer(f, "v_codes", v_codes, tokens * v_record_bytes)
+    for name, alpha in (("k_alpha", k_alpha), ("v_alpha", v_alpha)):
+        if alpha.element_size() != 2:
+            _refuse(f, f"{name} must be of a 16-bit type")
+        _buffer(f, name, alpha, 2 * tokens)
     t, _ = _table(f, table, device)
     status = entry_point(f)(
         dev_params_k.data_ptr(), dev_params_v.data_ptr(), batch, n_q_heads, n_kv_heads, HEAD_DIM,

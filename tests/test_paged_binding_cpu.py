@@ -95,3 +95,25 @@ def test_page_tables_on_another_device(calls, monkeypatch, name):
             _calls_with(table)[name]()
         assert e.value.status == 1 and "device" in str(e.value)
     assert len(calls) == 2
+
+
+def test_joined_attention_buffers(calls):
+    """Types and sizes of what the call reads: codes, scales, parameters and queries."""
+    good = _joined()
+    P.aatc_decode_attention_paged(**good)
+    P.aatc_decode_attention_paged(**{**good, "k_alpha": good["k_alpha"].view(torch.float16)})
+    assert len(calls) == 2
+    u8 = lambda *s: _on(torch.zeros(*s, dtype=torch.uint8))                      # noqa: E731
+    params = good["dev_params_k"].numel()
+    bad = [dict(dev_params_k=u8(params - 1)), dict(dev_params_v=u8(params - 1)), dict(k_codes=u8(2, 2, 63, 44)),
+           dict(v_codes=u8(1, 2, 1, 64 * 44)), dict(k_codes=_on(torch.zeros(2, 2, 64, 88, dtype=torch.uint8)[..., ::2], 0)),
+           dict(k_record_bytes=48), dict(v_record_bytes=48), dict(cap=128), dict(k_alpha=_floats(2, 2, 64)),
+           dict(v_alpha=_on(torch.zeros(2, 2, 63, dtype=torch.int16))), dict(k_alpha=u8(2, 2, 128)),
+           dict(q=_floats(1, 4, 128)), dict(q=_floats(2, 6, 128)[:, :4]), dict(q=_floats(4, 2, 128).transpose(0, 1)),
+           dict(k_codes=_on(torch.zeros(2, 2, 64, 44, dtype=torch.uint8), 1)), dict(seq_len=_i32(1)),
+           dict(page_len=_i32(2).long()), dict(out=_floats(2, 3, 128))]
+    for change in bad:
+        with pytest.raises(P.AatcError) as e:
+            P.aatc_decode_attention_paged(**{**good, **change})
+        assert e.value.status == 1, change
+    assert len(calls) == 2
