@@ -127,6 +127,15 @@ def _list(func: str, name: str, t, n: int):
         _refuse(func, f"{name} must be a contiguous int32 tensor of at least {n}")
 
 
+def _pairs(func: str, pairs) -> int:
+    """The number of pairs of an int32 tensor [n][2]."""
+    n = len(pairs)
+    if n and (pairs.dim() != 2 or pairs.shape[1] != 2):
+        _refuse(func, "pairs must be an int32 tensor [n][2]")
+    _list(func, "pairs", pairs, 2 * n)
+    return n
+
+
 def _floats(func: str, name: str, t, n: int):
     if t.dtype != _TORCH.float32 or not t.is_contiguous() or t.numel() < n:
         _refuse(func, f"{name} must be a contiguous float32 tensor of at least {n}")
@@ -348,8 +357,7 @@ def aatc_pages_fork(src_table, dst_table, ref, pairs, stream=None):
     """dst_table's rows pairs[:, 1] become copies of src_table's rows pairs[:, 0]."""
     f = "aatc_pages_fork"
     device = _on_device(f, ref, pairs)
-    n = len(pairs)
-    _list(f, "pairs", pairs, 2 * n)
+    n = _pairs(f, pairs)
     _list(f, "ref", ref, 1)
     src, _ = _table(f, src_table, device)
     dst, _ = _table(f, dst_table, device)
@@ -425,8 +433,7 @@ def aatc_pages_copy(pools, pairs, n_pairs=None, stream=None):
     contiguous); n_pairs: int32 tensor [1], copy no more pairs than that."""
     f = "aatc_pages_copy"
     device = _on_device(f, pools, pairs, n_pairs)
-    n = len(pairs)
-    _list(f, "pairs", pairs, 2 * n)
+    n = _pairs(f, pairs)
     if n_pairs is not None:
         _list(f, "n_pairs", n_pairs, 1)
     if pools.dim() < 3 or not (pools.is_contiguous() or pools[0].is_contiguous()):

@@ -117,3 +117,20 @@ def test_joined_attention_buffers(calls):
             P.aatc_decode_attention_paged(**{**good, **change})
         assert e.value.status == 1, change
     assert len(calls) == 2
+
+
+def test_lists_of_pairs(calls):
+    """[n][2], or nothing at all: rows of other lengths would be read as other pairs."""
+    pools = _on(torch.zeros(1, 4, 8, dtype=torch.int32))
+    fork = lambda pairs: P.aatc_pages_fork(_i32(4, 3), _i32(4, 3), _i32(9), pairs)       # noqa: E731
+    copy = lambda pairs: P.aatc_pages_copy(pools, pairs)                                  # noqa: E731
+    for call in (fork, copy):
+        call(_i32(3, 2))
+        call(_i32(0, 2))
+        call(_i32(0))
+        made = len(calls)
+        for bad in (_i32(3, 3), _i32(3, 4), _i32(3, 2, 2), _i32(6), _i32(3, 1), _i32(3, 2).long(),
+                    _on(torch.zeros(3, 4, dtype=torch.int32)[:, ::2])):
+            with pytest.raises(P.AatcError):
+                call(bad)
+        assert len(calls) == made
