@@ -292,7 +292,8 @@ def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n
                                 window: int = 0, sink: int = 0, softcap: float = 0.0, slopes=None,
                                 lse=None, stream=None):
     """Attention of one token per sequence (q: [batch][n_q_heads][128], rows q_stride elements
-    apart) over the pages; out [batch][n_q_heads][128] and lse [batch][n_q_heads] in float32."""
+    apart, by default as the tensor has them) over the pages; out [batch][n_q_heads][128] and lse
+    [batch][n_q_heads] in float32."""
     f = "aatc_paged_decode_attention"
     device = _on_device(f, seq_len, q, out, workspace, slopes, lse, cache.tensors[0])
     _list(f, "seq_len", seq_len, batch)
@@ -302,6 +303,10 @@ def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n
     if slopes is not None:
         _floats(f, "slopes", slopes, n_q_heads)
     stride = n_q_heads * HEAD_DIM if q_stride is None else q_stride
+    if q_stride is None and batch > 1 and not q.is_contiguous():
+        if q.shape[0] < batch:
+            _refuse(f, f"q has {q.shape[0]} rows of {batch}")
+        stride = q.stride(0)
     _tokens(f, "q", q, batch, stride, n_q_heads)
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), batch, n_q_heads, q.data_ptr(),

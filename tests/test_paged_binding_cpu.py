@@ -134,3 +134,28 @@ def test_lists_of_pairs(calls):
             with pytest.raises(P.AatcError):
                 call(bad)
         assert len(calls) == made
+
+
+def test_rows_of_queries(monkeypatch, calls):
+    """Without q_stride rows lie as the tensor has them, the heads of a wider projection too."""
+    got = []
+    monkeypatch.setattr(_paged, "entry_point", lambda name: lambda *a: got.append(a[7]) or 0)
+
+    def stride_of(q, batch, **more):
+        P.aatc_paged_decode_attention(_cache(), _i32(3, 3), _i32(3), batch, 4, q, 0.1, _floats(3, 4, 128),
+                                      _space(), **more)
+        return got[-1]
+    wide = _floats(3, 8, 128)
+    assert stride_of(_floats(3, 4, 128), 3) == 512
+    assert stride_of(_floats(12, 128), 3) == 512
+    assert stride_of(_floats(4 * 3 * 128), 3) == 512
+    assert stride_of(wide[:, :4], 3) == 1024 and stride_of(wide[:, 4:], 3) == 1024
+    assert stride_of(wide.reshape(3, 1024)[:, 512:], 3) == 1024
+    assert stride_of(wide[:, 4:], 1) == 512                 # (one row: any)
+    assert stride_of(wide[:, 4:], 3, q_stride=1024) == 1024
+    assert stride_of(wide, 3, q_stride=1024) == 1024
+    for bad in (_floats(4, 3, 128).transpose(0, 1), _floats(3, 4, 256)[..., ::2], wide[:2, :4]):
+        made = len(got)
+        with pytest.raises(P.AatcError):
+            stride_of(bad, 3)
+        assert len(got) == made
