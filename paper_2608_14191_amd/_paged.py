@@ -281,6 +281,13 @@ def aatc_paged_decode_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: in
     return int(entry_point("aatc_paged_decode_workspace_bytes")(batch, n_q_heads, n_kv_heads))
 
 
+def _space(func: str, workspace) -> int:
+    """The bytes of a workspace, for the C side to compare with what the call needs."""
+    if not workspace.is_contiguous():
+        _refuse(func, "the workspace must be a contiguous tensor")
+    return workspace.nbytes
+
+
 def _buffer(func: str, name: str, t, n: int):
     """A contiguous tensor of any type that holds n bytes."""
     if not t.is_contiguous() or t.nbytes < n:
@@ -311,7 +318,7 @@ def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), batch, n_q_heads, q.data_ptr(),
                             _dtype(q), stride, softmax_scale, window, sink, softcap, _ptr(slopes),
-                            out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+                            out.data_ptr(), _ptr(lse), workspace.data_ptr(), _space(f, workspace),
                             _raw_stream(device) if stream is None else int(stream))
     if status:
         raise AatcError(f, status)
@@ -351,7 +358,7 @@ def aatc_decode_attention_paged(dev_params_k, dev_params_v, batch: int, n_q_head
         q.data_ptr(), _dtype(q), k_codes.data_ptr(), k_alpha.data_ptr(), v_codes.data_ptr(),
         v_alpha.data_ptr(), seq_len.data_ptr(), cap, k_record_bytes, v_record_bytes, softmax_scale,
         cache.address, t, page_len.data_ptr(), out.data_ptr(), workspace.data_ptr(),
-        workspace.nbytes, _raw_stream(device) if stream is None else int(stream))
+        _space(f, workspace), _raw_stream(device) if stream is None else int(stream))
     if status:
         raise AatcError(f, status)
 
@@ -408,7 +415,7 @@ def aatc_pages_reserve(table, ref, page_tokens: int, held, wanted, pairs, lackin
     _list(f, "pairs", pairs, 2 * rows)
     status = entry_point(f)(t, ref.data_ptr(), ref.numel(), page_tokens, held.data_ptr(),
                             wanted.data_ptr(), pairs.data_ptr(), lacking.data_ptr(),
-                            workspace.data_ptr(), workspace.nbytes,
+                            workspace.data_ptr(), _space(f, workspace),
                             _raw_stream(device) if stream is None else int(stream))
     if status:
         raise AatcError(f, status)
@@ -427,7 +434,7 @@ def aatc_pages_compact(table, ref, table_out, ref_out, pairs, moves, workspace, 
     t, _ = _table(f, table, device)
     o, _ = _table(f, table_out, device)
     status = entry_point(f)(t, ref.data_ptr(), n_pages, o, ref_out.data_ptr(), pairs.data_ptr(),
-                            moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                            moves.data_ptr(), workspace.data_ptr(), _space(f, workspace),
                             _raw_stream(device) if stream is None else int(stream))
     if status:
         raise AatcError(f, status)

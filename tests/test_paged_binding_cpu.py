@@ -159,3 +159,18 @@ def test_rows_of_queries(monkeypatch, calls):
         with pytest.raises(P.AatcError):
             stride_of(bad, 3)
         assert len(got) == made
+
+
+def test_workspaces_are_contiguous(calls):
+    """(An expanded tensor has more elements than memory.)"""
+    for bad in (_on(torch.zeros(1, dtype=torch.uint8).expand(1 << 20)), _on(torch.zeros(64, dtype=torch.uint8)[::2])):
+        with pytest.raises(P.AatcError):
+            P.aatc_paged_decode_attention(_cache(), _i32(3, 3), _i32(3), 3, 4, _floats(3, 4, 128), 0.1,
+                                          _floats(3, 4, 128), bad)
+        with pytest.raises(P.AatcError):
+            P.aatc_decode_attention_paged(**{**_joined(), "workspace": bad})
+        with pytest.raises(P.AatcError):
+            P.aatc_pages_reserve(_i32(2, 3), _i32(4), 16, _i32(2), _i32(2), _i32(2, 2), _i32(1), bad)
+        with pytest.raises(P.AatcError):
+            P.aatc_pages_compact(_i32(2, 3), _i32(4), _i32(2, 3), _i32(4), _i32(2, 2), _i32(1), bad)
+    assert calls == []
