@@ -158,7 +158,7 @@ aatc_status aatc_paged_append(const aatc_paged_cache* cache, const aatc_page_tab
  * q         device, sequence b at q + b * q_stride elements, [n_q_heads][d] contiguous; F32,
  *           BF16 or F16.
  * window    0: none.  sink: tokens at the start that stay attended with a window, >= 0.
- * softcap   0: none, else > 0 (and softmax_scale / softcap finite).
+ * softcap   0: none, else > 0 (and softmax_scale / softcap finite); from 1e30 on none either.
  * slopes    device [n_q_heads] fp32 (a bias that falls with distance) or NULL.
  * out       device [batch][n_q_heads][d] fp32, 16-byte aligned.
  * lse       device [batch][n_q_heads] fp32 or NULL.

@@ -17,6 +17,10 @@ constexpr int64_t kMaxPages = INT32_MAX;
 constexpr int64_t kMaxList = (int64_t)1 << 30;        // tokens or pairs of one call
 constexpr int64_t kMaxRows = ((int64_t)1 << 24) - 1;  // rows listed: a workgroup of 256 each
 
+// Caps from here on change no score (below 1e26 tanh(z / cap) is z / cap in float32, and a softmax
+// with larger ones has only zeros and ones), but their products pass float32's range.
+constexpr float kNoCap = 1e30f;
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool known(aatc_dtype t) { return t == AATC_F32 || t == AATC_BF16 || t == AATC_F16; }
 int size_of(aatc_dtype t) { return t == AATC_F32 ? 4 : 2; }
@@ -278,7 +282,7 @@ extern "C" aatc_status aatc_paged_decode_attention(
                              softmax_scale);
     a.window = window;
     a.sink = sink;
-    a.cap = softcap;
+    a.cap = softcap < kNoCap ? softcap : 0.f;
     a.slopes = slopes;
     a.out = out;
     a.lse = lse;

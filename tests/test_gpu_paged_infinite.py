@@ -176,3 +176,14 @@ def test_joined_every_score_minus_infinity(hq):
     assert torch.all(got[3] == 0)
     # (the other heads: the compressed path's own errors, 2e-5)
     assert (got[:, 1:] - before[:, 1:]).norm() <= 2e-5 * before[:, 1:].norm()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f16", "f32"])
+def test_caps_past_every_score(cache):
+    """A cap as large as float32 allows is none."""
+    case = _case(7, [100, 900], 4, 2, cache, cache)
+    want, want_lse = _run(*case)
+    for cap in (1e25, 9e29, 1e30, 1e38, 3.4e38):
+        got, lse = _run(*case, softcap=cap)
+        _finite_alike(got, want.double())
+        assert torch.all((lse - want_lse).abs() <= 2.0 ** -20 * (1 + want_lse.abs()))
