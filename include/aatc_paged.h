@@ -211,14 +211,14 @@ aatc_status aatc_decode_attention_paged(
  * (the same or another table, of as many entries per row), and their pages' counts go up: beams
  * and samples share what they have in common.  What the dst rows held is forgotten (not freed).
  * A dst row listed twice takes the last of its sources; rows outside the tables are skipped; no
- * row may be a source and a destination of one call.  n < 2^24, as for aatc_pages_free (more:
- * AATC_E_UNSUPPORTED).
+ * row may be a source and a destination of one call.  n at most 2^18 (more: AATC_E_UNSUPPORTED):
+ * every pair is compared with all later ones (32768 pairs 1.5 ms).
  */
 aatc_status aatc_pages_fork(const aatc_page_table* src, const aatc_page_table* dst, int32_t* ref,
                             int64_t n_pages, const int32_t* pairs, int64_t n, void* stream);
 
 /* aatc_pages_free -- empties the rows listed (device [n] int32; twice does no harm): the counts
- * of their pages go down and the entries become -1. */
+ * of their pages go down and the entries become -1.  n < 2^24 (more: AATC_E_UNSUPPORTED). */
 aatc_status aatc_pages_free(const aatc_page_table* table, int32_t* ref, int64_t n_pages,
                             const int32_t* rows, int64_t n, void* stream);
 

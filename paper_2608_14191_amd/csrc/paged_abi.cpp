@@ -16,6 +16,7 @@ namespace {
 constexpr int64_t kMaxPages = INT32_MAX;
 constexpr int64_t kMaxList = (int64_t)1 << 30;        // tokens or pairs of one call
 constexpr int64_t kMaxRows = ((int64_t)1 << 24) - 1;  // rows listed: a workgroup of 256 each
+constexpr int64_t kMaxForks = (int64_t)1 << 18;       // pairs, each compared with all later ones
 
 // Caps from here on change no score (below 1e26 tanh(z / cap) is z / cap in float32, and a softmax
 // with larger ones has only zeros and ones), but their products pass float32's range.
@@ -347,7 +348,7 @@ extern "C" aatc_status aatc_pages_fork(const aatc_page_table* src, const aatc_pa
     if (src->max_pages != dst->max_pages || n < 0 || n > kMaxList || !pairs || !aligned(pairs, 4))
       return AATC_E_INVALID;
     if (n == 0) return AATC_OK;
-    if (n > kMaxRows) return AATC_E_UNSUPPORTED;
+    if (n > kMaxForks) return AATC_E_UNSUPPORTED;
     return launch_pages_fork(*src, *dst, ref, n_pages, pairs, n, stream);
   } catch (...) {
     return AATC_E_INVALID;

@@ -5,6 +5,7 @@ import torch
 
 import paper_2608_14191_amd as P
 from paper_2608_14191_amd import _paged
+from test_paged_cpu import A, TABLE, UNSUPPORTED, _call
 
 
 class _On(torch.Tensor):
@@ -174,3 +175,10 @@ def test_workspaces_are_contiguous(calls):
         with pytest.raises(P.AatcError):
             P.aatc_pages_compact(_i32(2, 3), _i32(4), _i32(2, 3), _i32(4), _i32(2, 2), _i32(1), bad)
     assert calls == []
+
+
+def test_forks_of_one_call():
+    """The work grows with the square of the pairs: 2^18 at most (2^24 took minutes)."""
+    fork = dict(src=(P.PageTable, TABLE), dst=(P.PageTable, TABLE), ref=A, n_pages=100, pairs=A, n=0, stream=None)
+    for n in ((1 << 18) + 1, 1 << 20, (1 << 24) - 1, 1 << 24):
+        assert _call("aatc_pages_fork", fork, n=n) == UNSUPPORTED
