@@ -34,9 +34,10 @@ namespace aatc {
 namespace {
 
 // Runs (few rows): eight waves a workgroup, one workgroup a compute unit, so that a row has few
-// parts to join (1 x 32768 tokens, 8 KV heads: 31.2 us, with four waves and twice as many 34.0).
+// parts to join (1 x 32768 tokens, 8 KV heads, float16: 27.7 us, with four waves and twice as many
+// 30.5; shorter rows would gain by those: 1 x 4000 bf16 13.0 and 10.7).
 // Lines (many rows): four waves, two workgroups a compute unit, whose row changes cover each
-// other (48 x 2052 tokens, 8 KV heads, float32: 144.5 us, with eight waves 159.9).
+// other (48 x 2052 tokens, 8 KV heads, float32: 142.2 us, with eight waves 156.3).
 constexpr int kRunWaves = 8, kRunGroups = 256;
 constexpr int kLineWaves = 4, kLineGroups = 512;
 constexpr int kMaxRunRows = 256;                  // a workgroup each at least
@@ -94,8 +95,9 @@ __device__ inline void load_queries(const void* q, int dtype, int64_t i, bool on
 }
 
 // FAR: keys and values are loaded past the caches.  Pools that do not fit there have nothing to
-// gain from them (4 x 131072 tokens, 8 KV heads: 323 us, 362 through the caches; 1 x 32768 28.8
-// and 31.8), smaller ones may be found there again (1 x 4000 tokens 14.4 and 12.8).
+// gain from them (4 x 131072 tokens, 8 KV heads: 317.5 us, 358 through the caches; 1 x 32768 27.7
+// and 30.7), smaller ones may be found there again (1 x 4000 tokens 14.7 and 13.0).  The pool is what
+// counts, whatever part of it the sequences have.
 constexpr int64_t kFarBytes = (int64_t)128 << 20;
 template <bool FAR, class V>
 __device__ inline V load16(const char* p) {
@@ -458,7 +460,7 @@ __device__ inline Row row_of(const PagedArgs& a, int seq, int row) {
 
 // A wave's way through its rows.  Where a workgroup has several, the pages of the next one's first
 // tiles are fetched before a row is begun, and its queries, keys and values when that is done, under
-// the row's join (192 rows of 63 tiles at most: 43.7 us, 50.8 without).
+// the row's join (192 rows of 63 tiles at most, as lines: 44.2 us, 46.4 without).
 template <class M, int QT>
 struct Walk {
   static constexpr int TT = M::kTokens, NM = M::kMine;
@@ -1000,9 +1002,9 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
   const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads * a.hg;
   const int64_t most = rows * std::max(1, (a.len_max + tt - 1) / tt);
-  // Runs for up to half the grid's rows, or up to all of it where no row can be long (one run a row
-  // then lasts as long as the longest: 256 rows up to 2000 tokens 41.1 us, as lines 51.1; 240 rows up
-  // to 12000 tokens 201.7, as lines 161.8).
+  // Runs for up to half the grid's rows, or up to all of it where no row can be long, by the width of
+  // the table (one run a row then lasts as long as the longest: 256 rows up to 2000 tokens 41.4 us,
+  // as lines 52.0; 240 rows up to 12000 tokens 201, as lines 161).
   const bool runs = rows <= kRunGroups / 2 || (rows <= kMaxRunRows && a.len_max <= 128 * tt);
   a.slot_heads = std::min(a.G, kPagedHeads);
   a.parts_bytes = (int)parts_bytes(rows, a.slot_heads);

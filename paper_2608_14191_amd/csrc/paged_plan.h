@@ -73,9 +73,9 @@ AATC_PAGED_HD inline int run_begin(int n, int runs, int i) { return (int)((int64
 //
 // To begin a row, and to join its parts, takes a wave about as long as five tiles each.  So rows
 // stay whole, a wave each, where there are waves enough and the longest is not much over the
-// average share (1544 rows of 13 tiles at most: 68 us shared by workgroups), or a workgroup each.
-// Else waves for themselves, unless rows would be cut into many parts (784 rows of 60 tiles at
-// most: 126 us by waves, 114 by workgroups).
+// average share (1544 rows of 13 tiles at most: 57.4 us, 58.9 shared by workgroups), or a workgroup
+// each.  Else waves for themselves, unless rows would be cut into many parts (784 rows of 60 tiles at
+// most: 104.8 us by waves, 97.0 by workgroups).
 struct LineWay {
   int quota;
   bool waves, whole;

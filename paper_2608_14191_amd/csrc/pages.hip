@@ -124,10 +124,11 @@ __global__ __launch_bounds__(kListThreads) void free_kernel(int32_t* table, int6
 // of free pages in the order of the claims.
 //
 // The rows' first claims, the wants and the free pages are in LDS as far as they fit (the round trips
-// to memory are the time: 128 children of 32 parents 12.0 us with all of them in the workspace), else
-// in the workspace, which also counts the earlier claims of a page over several steps.  Where no row
-// has two claims (a decode step) claim i is row i's; else they are numbered by a scan and found by a
-// search, four a thread and step where they are many.
+// to memory are the time), else in the workspace, which also counts the earlier claims of a page over
+// several steps.  Where no row has two claims (a decode step) claim i is row i's; else they are
+// numbered by a scan and found by a search, four a thread and step where they are many.  64 rows of a
+// new page each in a pool of 4096 5.6 us (6.3 with the scan and the search), 8192 pages of one row
+// 19.0 (24.5 with one claim a thread and step).
 struct ReserveSpace {
   int32_t *first, *row, *entry, *free;
 };
@@ -398,7 +399,9 @@ constexpr int kCopyUnroll = 4;
 constexpr int64_t kCopyPiece = 16 * kListThreads * kCopyUnroll;
 
 // FAR: past the caches (copies that would not stay in them: 2048 pages of 32 KiB in eight pools
-// 101.7 us, 109.2 through the caches; 128 pages of 64 KiB in sixteen 44.5, 37.2 through them).
+// 212.5 us, 218.4 through the caches; 128 copies of pages of 64 KiB that children share, in sixteen
+// pools, with the three launches before them 58.2, 51.9 through them).  All listed pairs count,
+// whether they copy or not: how many do, only the device knows.
 constexpr int64_t kFarBytes = (int64_t)512 << 20;
 template <bool FAR>
 __global__ __launch_bounds__(kListThreads) void copy_kernel(char* base, int64_t n_pools,
@@ -447,9 +450,9 @@ aatc_status launch_pages_copy(void* base, int64_t n_pools, int64_t pool_stride, 
   const int64_t cap = (int64_t)1 << 14;
   const int64_t grid = n > cap || pieces > cap ? cap : std::min(cap, n * n_pools * pieces);
   const bool far = 2.0 * (double)n * (double)n_pools * (double)page_bytes > (double)kFarBytes;
-  hipLaunchKernelGGL(far ? copy_kernel<true> : copy_kernel<false>, dim3((unsigned)grid), dim3(kListThreads), 0,
-                     (hipStream_t)stream, static_cast<char*>(base), n_pools, pool_stride,
-                     (int)n_pages, page_bytes, pairs, n, n_dev);
+  hipLaunchKernelGGL(far ? copy_kernel<true> : copy_kernel<false>, dim3((unsigned)grid),
+                     dim3(kListThreads), 0, (hipStream_t)stream, static_cast<char*>(base), n_pools,
+                     pool_stride, (int)n_pages, page_bytes, pairs, n, n_dev);
   return done();
 }
 
@@ -481,7 +484,8 @@ aatc_status launch_pages_reserve(const aatc_page_table& t, int32_t* ref, int64_t
   const bool few = n_pages <= kPlanThreads * kFewPages;
   hipLaunchKernelGGL(few ? reserve_kernel<kFewPages> : reserve_kernel<kManyPages>, dim3(1),
                      dim3(kPlanThreads), 0, (hipStream_t)stream, t.table, t.stride, t.rows, ref,
-                     (int)n_pages, log2_of(page_tokens), len_max, held, wanted, pairs, lacking, workspace);
+                     (int)n_pages, log2_of(page_tokens), len_max, held, wanted, pairs, lacking,
+                     workspace);
   return done();
 }
 
@@ -491,8 +495,8 @@ aatc_status launch_pages_compact(const aatc_page_table& t, const int32_t* ref, i
   const hipStream_t st = (hipStream_t)stream;
   auto* to = static_cast<int32_t*>(workspace);
   const bool few = n_pages <= kPlanThreads * kFewPages;
-  hipLaunchKernelGGL(few ? compact_plan_kernel<kFewPages> : compact_plan_kernel<kManyPages>, dim3(1), dim3(kPlanThreads), 0, st, ref, (int)n_pages,
-                     ref_out, pairs, moves, to);
+  hipLaunchKernelGGL(few ? compact_plan_kernel<kFewPages> : compact_plan_kernel<kManyPages>, dim3(1),
+                     dim3(kPlanThreads), 0, st, ref, (int)n_pages, ref_out, pairs, moves, to);
   if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
   const int64_t all = (int64_t)t.rows * t.max_pages;
   const int64_t grid = std::min<int64_t>((all + kListThreads - 1) / kListThreads, 2048);

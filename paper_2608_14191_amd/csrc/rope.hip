@@ -61,8 +61,7 @@ struct alignas(sizeof(T) * E < 16 ? sizeof(T) * E : 16) Chunk {
 };
 
 // FAR: past the caches (tokens that would not stay in them: 65536 of eight float32 heads
-// 98.2 us, 105.5 through the caches, 99.4 if only the stores pass; 4096 tokens of 32 bf16 heads with
-// the stores passing 12.8, 12.5 through them).
+// 98.7 us, 104.4 through the caches; 4096 tokens of 32 bf16 heads 15.5, 12.7 through them).
 template <bool FAR, class C>
 __device__ inline void put_chunk(void* p, const C& c) {
   if constexpr (FAR && sizeof(C) == 16)
@@ -89,7 +88,7 @@ __device__ inline void wave_sync() {
 // How a head's row is moved.  Whole: in 16-byte chunks, with a lane's partners in a chunk of its own
 // (rows 16-byte aligned, and half a multiple of a chunk's elements unless pairs are interleaved).
 // Shuffled: in chunks, the partners by way of LDS (half of any size: 32534 tokens of eight bf16
-// heads, 2 channels rotated, 75.3 us channel by channel, 38.5 so).  Single: channel by channel
+// heads, 2 channels rotated, 75.0 us channel by channel, 39.2 so).  Single: channel by channel
 // (rows of any alignment).
 enum Path { kWhole, kShuffled, kSingle };
 

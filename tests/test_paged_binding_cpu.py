@@ -178,7 +178,7 @@ def test_workspaces_are_contiguous(calls):
 
 
 def test_forks_of_one_call():
-    """The work grows with the square of the pairs: 2^18 at most (2^24 took minutes)."""
+    """The work grows with the square of the pairs: 2^18 at most (2^24 would take minutes)."""
     fork = dict(src=(P.PageTable, TABLE), dst=(P.PageTable, TABLE), ref=A, n_pages=100, pairs=A, n=0, stream=None)
     for n in ((1 << 18) + 1, 1 << 20, (1 << 24) - 1, 1 << 24):
         assert _call("aatc_pages_fork", fork, n=n) == UNSUPPORTED
