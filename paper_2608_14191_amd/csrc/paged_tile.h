@@ -1,0 +1,294 @@
+// A wave's tile of the attention over pages: 32 tokens (16 in float32) of one KV head against up to
+// 16 queries, scores = K Q^T and then O^T += V^T P^T on the matrix cores (paged.hip says how the two
+// fit together).  Device code of the kernels that read pages.
+#pragma once
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+
+#include "aatc.h"
+#include "params.h"
+
+namespace aatc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The maximum of a part that has attended tokens, all with scores of -infinity (a part without
+// attended tokens has -infinity and the sum 0).  Its sum is not 0, so that a head without any finite
+// score ends as the NaN that its softmax is; beside finite scores it has no weight.
+constexpr float kLowest = -FLT_MAX;
+constexpr int kRsrcWord3 = 0x00020000;            // raw buffer descriptor word 3 (gfx950)
+constexpr int kCoherent = 16;                     // cache policy sc1: device-coherent access
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// Lane l with lane l ^ 16, l ^ 32.
+__device__ inline float over_groups_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float over_groups_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// N consecutive query elements from element i on (aligned to the element only).
+template <class T, int N>
+struct Run {
+  T e[N];
+};
+template <int N>
+__device__ inline void load_queries(const void* q, int dtype, int64_t i, bool on, float (&x)[N]) {
+  Run<float, N> f;
+  Run<__bf16, N> b;
+  Run<_Float16, N> h;
+  if (dtype == AATC_F32) __builtin_memcpy(&f, static_cast<const float*>(q) + i, sizeof f);
+  else if (dtype == AATC_BF16) __builtin_memcpy(&b, static_cast<const __bf16*>(q) + i, sizeof b);
+  else __builtin_memcpy(&h, static_cast<const _Float16*>(q) + i, sizeof h);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float v = dtype == AATC_F32 ? f.e[e] : dtype == AATC_BF16 ? (float)b.e[e] : (float)h.e[e];
+    x[e] = on ? v : 0.f;
+  }
+}
+
+// FAR: keys and values are loaded past the caches.  Pools that do not fit there have nothing to
+// gain from them (4 x 131072 tokens, 8 KV heads: 317.5 us, 358 through the caches; 1 x 32768 27.7
+// and 30.7), smaller ones may be found there again (1 x 4000 tokens 14.7 and 13.0).  The pool is what
+// counts, whatever part of it the sequences have.
+constexpr int64_t kFarBytes = (int64_t)128 << 20;
+template <bool FAR, class V>
+__device__ inline V load16(const char* p) {
+  if constexpr (FAR) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+
+// The two products on 16-bit types.  A lane's place: n = lane % 16, g = lane / 16.
+template <class T, bool FAR>
+struct Half16 {
+  static constexpr bool kF16 = sizeof(T) == 2 && __is_same(T, _Float16);
+  typedef T v8 __attribute__((ext_vector_type(8)));
+  static constexpr int kTokens = 32;              // of a tile
+  static constexpr int kMine = 8;                 // scores of a lane: tokens 8 g .. 8 g + 7
+  static constexpr int kTerms = kF16 ? 2 : 3;     // of P
+  static constexpr float kLower = kF16 ? 14.f : 0.f;
+  // Token of the tile whose key chunk u (of two) lane (n, g) loads, and the 8-token block that
+  // a lane's keys and values are in.
+  static __device__ int key_token(int u, int n) { return 8 * (n >> 2) + 4 * u + (n & 3); }
+  static __device__ int key_block(int n) { return n >> 2; }
+  static __device__ int value_block(int g) { return g; }
+
+  static __device__ v4f mfma(v8 a, v8 b, v4f c) {
+    if constexpr (kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+
+  // Queries as terms: lane (n, g) holds head n's channels 8 (4 kk + g) .. + 7.
+  template <int QT>
+  struct Query {
+    v8 t[QT][4];
+    float back;                                   // head n's scores times this
+    __device__ void load(const void* q, int dtype, int64_t at, bool on, int g) {
+      if constexpr (QT == 1) {
+        back = 1.f;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          v4u x;
+          __builtin_memcpy(&x, static_cast<const T*>(q) + at + 8 * (4 * kk + g), 16);
+          t[0][kk] = __builtin_bit_cast(v8, on ? x : (v4u){0u, 0u, 0u, 0u});
+        }
+      } else {
+        float x[4][8], top = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          load_queries(q, dtype, at + 8 * (4 * kk + g), on, x[kk]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[kk][e]));
+        }
+        // f16 holds the terms of a head whose largest channel is near 2^15, down to 2^-39 of it.
+        int up = 0;
+        if constexpr (kF16) {
+          top = over_groups_max(top);
+          if (top > 0.f && top < INFINITY) up = 14 - ilogbf(top);
+          up = max(-126, min(126, up));
+        }
+        back = ldexpf(1.f, -up);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float r = kF16 ? ldexpf(x[kk][e], up) : x[kk][e];
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+              t[i][kk][e] = (T)r;
+              r -= (float)t[i][kk][e];
+            }
+          }
+      }
+    }
+  };
+
+  struct Keys {
+    v4u r[2][4];
+    // row(u): the lane's row of chunk u
+    __device__ void load(const char* row0, int64_t tok_stride, int g) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          r[u][kk] = load16<FAR, v4u>(row0 + u * 4 * tok_stride + 64 * kk + 16 * g);
+    }
+  };
+  struct Values {
+    v4u r[8];
+    __device__ void load(const char* row0, int64_t tok_stride, int n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        r[e] = load16<FAR, v4u>(row0 + e * tok_stride + 16 * n);
+    }
+    // Token e of the lane's counts as zeros unless `on` (0 times what is stored there may be NaN).
+    __device__ void keep(int e, bool on) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[e][i] = on ? r[e][i] : 0u;
+    }
+  };
+
+  template <int QT>
+  static __device__ void scores(const Keys& k, const Query<QT>& q, float (&z)[kMine]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      v4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = QT - 1; i >= 0; --i)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          s = mfma(__builtin_bit_cast(v8, k.r[u][kk]), q.t[i][kk], s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i] * q.back;
+    }
+  }
+
+  // acc[j][i]: channel 8 (4 g + i) + j of head n.
+  static __device__ int channel(int j, int i, int g) { return 8 * (4 * g + i) + j; }
+  static __device__ void accumulate(const Values& v, const float (&p)[kMine], v4f (&acc)[8]) {
+    v8 t[kTerms];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float r = p[e];
+#pragma unroll
+      for (int i = 0; i < kTerms; ++i) {
+        t[i][e] = (T)r;
+        r -= (float)t[i][e];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v4u a;                                      // column j of the lane's 8 x 8 block
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        a[d] = __builtin_amdgcn_perm(v.r[2 * d + 1][j / 2], v.r[2 * d][j / 2],
+                                     j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int i = kTerms - 1; i >= 0; --i) acc[j] = mfma(__builtin_bit_cast(v8, a), t[i], acc[j]);
+    }
+  }
+};
+
+// The two products on float32 (v_mfma_f32_16x16x4_f32: no splitting).
+template <bool FAR>
+struct Full32 {
+  static constexpr int kTokens = 16;
+  static constexpr int kMine = 4;                 // tokens 4 g .. 4 g + 3
+  static constexpr float kLower = 0.f;
+  static __device__ int key_token(int, int n) { return n; }
+  static __device__ int key_block(int n) { return n >> 3; }
+  static __device__ int value_block(int g) { return g >> 1; }
+  static __device__ v4f mfma(float a, float b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+  }
+  template <int QT>
+  struct Query {                                  // channels 16 c + 4 g .. + 3
+    v4f t[8];
+    __device__ void load(const void* q, int dtype, int64_t at, bool on, int g) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float x[4];
+        load_queries(q, dtype, at + 16 * c + 4 * g, on, x);
+        t[c] = (v4f){x[0], x[1], x[2], x[3]};
+      }
+    }
+  };
+  struct Keys {
+    v4f r[8];
+    __device__ void load(const char* row0, int64_t, int g) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) r[c] = load16<FAR, v4f>(row0 + 64 * c + 16 * g);
+    }
+  };
+  struct Values {
+    v4f r[4][2];
+    __device__ void load(const char* row0, int64_t tok_stride, int n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          r[e][c] = load16<FAR, v4f>(row0 + e * tok_stride + 256 * c + 16 * n);
+    }
+    __device__ void keep(int e, bool on) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[e][c][i] = on ? r[e][c][i] : 0.f;
+    }
+  };
+  template <int QT>
+  static __device__ void scores(const Keys& k, const Query<QT>& q, float (&z)[kMine]) {
+    v4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = mfma(k.r[c][e], q.t[c][e], s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = s[i];
+  }
+  // acc[4 c + e][i]: channel 64 c + 4 (4 g + i) + e of head n.
+  static __device__ int channel(int j, int i, int g) {
+    return 64 * (j >> 2) + 4 * (4 * g + i) + (j & 3);
+  }
+  static __device__ void accumulate(const Values& v, const float (&p)[kMine], v4f (&acc)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[4 * c + e] = mfma(v.r[i][c][e], p[i], acc[4 * c + e]);
+  }
+};
+
+// tanh to a few ulps: for small |x| the first terms of its odd series (the next is 4e-8 of x at
+// 0.55), else from exp(-2 |x|).
+__device__ inline float tanh_of(float x) {
+  const float y = fabsf(x), s = y * y;
+  float r = 0.0014558343f;                         // 929569 / 638512875, 21844 / 6081075, ...
+  r = fmaf(-r, s, 0.003592128f);
+  r = fmaf(-r, s, 0.0088632356f);
+  r = fmaf(-r, s, 0.021869488f);
+  r = fmaf(-r, s, 0.053968254f);
+  r = fmaf(-r, s, 0.13333334f);
+  r = fmaf(-r, s, 0.33333334f);
+  const float small = fmaf(-r * s, y, y);
+  const float e = __builtin_amdgcn_exp2f(-2.f * kLog2e * y);
+  const float large = (1.f - e) / (1.f + e);
+  return copysignf(y < 0.55f ? small : large, x);
+}
+
+}  // namespace
+}  // namespace aatc
