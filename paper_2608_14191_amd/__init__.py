@@ -24,3 +24,9 @@ from ._paged import (  # noqa: F401
     aatc_pages_workspace_bytes, aatc_rope, aatc_rope_frequencies,
 )
 from ._lib import F16  # noqa: F401
+from ._drafts import (  # noqa: F401
+    MAX_DRAFTS, aatc_paged_tree_accept, aatc_paged_tree_attention, aatc_paged_tree_workspace_bytes,
+)
+from ._sparse import (  # noqa: F401
+    aatc_page_bounds, aatc_paged_sparse_attention, aatc_paged_sparse_workspace_bytes,
+)

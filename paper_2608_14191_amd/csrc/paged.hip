@@ -48,13 +48,6 @@ constexpr int kMaxRunRows = 256;                  // a workgroup each at least
 constexpr int kWorkers = kLineGroups * kLineWaves, kCounterStride = 64;
 constexpr size_t kCountersBytes = (size_t)kWorkers * kCounterStride * sizeof(unsigned);
 
-// What one wave has of a row: for head n of its lanes the maximum, the sum and the value sums
-// (acc[j][r]: channel M::channel(j, r, g)) over the tiles first, first + step .. below last.
-struct RowPart {
-  float m, l;
-  v4f acc[8];
-};
-
 // A row: query heads h0 .. h0 + heads - 1 of sequence `seq` on KV head `kvh`.
 struct Row {
   int len, kvh, h0, heads;

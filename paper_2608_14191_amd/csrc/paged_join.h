@@ -13,6 +13,13 @@ namespace {
 
 constexpr int kPagedHeads = 16;                   // query heads of a row
 
+// What one wave has of a row: for head n of its lanes the maximum, the sum and the value sums
+// (acc[j][r]: channel M::channel(j, r, g)) over the tiles first, first + step .. below last.
+struct RowPart {
+  float m, l;
+  v4f acc[8];
+};
+
 // LDS of the joins: the waves' sums, then (the same bytes) the weights of a row's parts; and the
 // sums over groups of them.
 template <int W, int GROUPS>

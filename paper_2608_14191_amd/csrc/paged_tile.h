@@ -75,6 +75,7 @@ __device__ inline V load16(const char* p) {
 template <class T, bool FAR>
 struct Half16 {
   static constexpr bool kF16 = sizeof(T) == 2 && __is_same(T, _Float16);
+  typedef T Elem;
   typedef T v8 __attribute__((ext_vector_type(8)));
   static constexpr int kTokens = 32;              // of a tile
   static constexpr int kMine = 8;                 // scores of a lane: tokens 8 g .. 8 g + 7
@@ -178,6 +179,66 @@ struct Half16 {
 
   // acc[j][i]: channel 8 (4 g + i) + j of head n.
   static __device__ int channel(int j, int i, int g) { return 8 * (4 * g + i) + j; }
+
+  // The product for several groups of 16 queries: the values are turned once.
+  struct Turned {
+    v4u a[8];
+  };
+  static __device__ void turn(const Values& v, Turned& t) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        t.a[j][d] = __builtin_amdgcn_perm(v.r[2 * d + 1][j / 2], v.r[2 * d][j / 2],
+                                          j & 1 ? 0x07060302u : 0x05040100u);
+  }
+  // P as terms of 8 tokens.  bf16: the upper half of the number, the upper half of the rest, the rest
+  // (exact: 8 bits each of 24).  f16: towards zero, then the rest to the nearest (2^-22 of it).
+  struct Weights {
+    v4u t[kTerms];
+  };
+  static __device__ Weights split(const float (&p)[kMine]) {
+    Weights w;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      float x = p[2 * d], y = p[2 * d + 1];
+      if constexpr (kF16) {
+        const auto top = __builtin_amdgcn_cvt_pkrtz(x, y);
+        typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+        const v2h rest = {(_Float16)(x - (float)top[0]), (_Float16)(y - (float)top[1])};
+        w.t[0][d] = __builtin_bit_cast(uint32_t, top);
+        w.t[1][d] = __builtin_bit_cast(uint32_t, rest);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kTerms; ++i) {
+          w.t[i][d] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+          x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+          y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        }
+      }
+    }
+    return w;
+  }
+  static __device__ v4f add(const Turned& v, int j, const Weights& w, v4f acc) {
+#pragma unroll
+    for (int i = kTerms - 1; i >= 0; --i)
+      acc = mfma(__builtin_bit_cast(v8, v.a[j]), __builtin_bit_cast(v8, w.t[i]), acc);
+    return acc;
+  }
+  // Token e in the place of the first, if asked.
+  static __device__ void take(Values& to, const Values& v, int e, bool on) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to.r[0][i] = on ? v.r[e][i] : to.r[0][i];
+  }
+  // Whether the lane's part of token e is not finite.
+  static __device__ bool bad(const Values& v, int e) {
+    const uint32_t up = kF16 ? 0x7c00u : 0x7f80u;
+    bool b = false;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      b |= ((v.r[e][d] & up) == up) | ((v.r[e][d] >> 16 & up) == up);
+    return b;
+  }
   static __device__ void accumulate(const Values& v, const float (&p)[kMine], v4f (&acc)[8]) {
     v8 t[kTerms];
 #pragma unroll
@@ -205,6 +266,7 @@ struct Half16 {
 // The two products on float32 (v_mfma_f32_16x16x4_f32: no splitting).
 template <bool FAR>
 struct Full32 {
+  typedef float Elem;
   static constexpr int kTokens = 16;
   static constexpr int kMine = 4;                 // tokens 4 g .. 4 g + 3
   static constexpr float kLower = 0.f;
@@ -262,6 +324,36 @@ struct Full32 {
   // acc[4 c + e][i]: channel 64 c + 4 (4 g + i) + e of head n.
   static __device__ int channel(int j, int i, int g) {
     return 64 * (j >> 2) + 4 * (4 * g + i) + (j & 3);
+  }
+  typedef Values Turned;
+  static __device__ void turn(const Values& v, Turned& t) { t = v; }
+  struct Weights {
+    float p[kMine];
+  };
+  static __device__ Weights split(const float (&p)[kMine]) {
+    Weights w;
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) w.p[e] = p[e];
+    return w;
+  }
+  static __device__ v4f add(const Turned& v, int j, const Weights& w, v4f acc) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) acc = mfma(v.r[i][j >> 2][j & 3], w.p[i], acc);
+    return acc;
+  }
+  static __device__ void take(Values& to, const Values& v, int e, bool on) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to.r[0][c][i] = on ? v.r[e][c][i] : to.r[0][c][i];
+  }
+  static __device__ bool bad(const Values& v, int e) {
+    bool b = false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b |= !(fabsf(v.r[e][c][i]) < INFINITY);
+    return b;
   }
   static __device__ void accumulate(const Values& v, const float (&p)[kMine], v4f (&acc)[8]) {
 #pragma unroll

@@ -1,0 +1,678 @@
+// Sparse attention over a paged cache: the pages' bounds, the pages that a query can score highest
+// in, and attention over those.
+//
+// A page's bound on a score sum_c q_c k_c is sum_c max(q_c hi_c, q_c lo_c), hi and lo the largest and
+// smallest value of channel c in the page: with the positive and the negative part of q a product of
+// 256 numbers, [q+ q-] . [hi lo].  All of them are held in 8 bits with powers of two as steps, so the
+// product on the int8 matrix cores, the steps and the comparison are exact: the pages picked depend on
+// no order of summation.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "paged_join.h"
+#include "paged_plan.h"
+#include "paged_tile.h"
+#include "params.h"
+#include "sparse.h"
+
+namespace aatc {
+namespace {
+
+constexpr int kLowestStep = -50, kHighestStep = 100;
+
+// The exponent of the smallest power of two, from 2^-50 on, of which 127 reach `top` (finite, >= 0).
+__device__ inline int step_of(float top) {
+  const uint32_t bits = __float_as_uint(top);
+  const int e = (int)(bits >> 23) - 126 - ((bits & 0x7fffffu) <= 0x7e0000u ? 7 : 6);
+  return max(e, kLowestStep);
+}
+__device__ inline float power_of_two(int e) {     // -126 <= e <= 127
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// --- bounds ---------------------------------------------------------------------------------------
+
+// A wave takes a page of a KV head at a time: a row of 16 (32 in float32) lanes has a token, a lane 16
+// bytes of it; what the rows have meets in row swaps.  Reads every key once: the memory bounds it.
+constexpr int kBoundWaves = 4, kBoundGroups = 2048;
+
+template <class T>
+__global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) {
+  constexpr int NT = 64 * kBoundWaves;
+  constexpr int N = 16 / sizeof(T), L = kD / N;    // channels of a lane, lanes of a token
+  __shared__ int before[NT];                       // pages of the threads' rows before
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int each = (a.rows + NT - 1) / NT;
+  auto tokens = [&](const int32_t* x, int b) { return x ? min(max(x[b], 0), a.len_max) : 0; };
+  // Pages that row b's new tokens fall into: `first` on, so many.
+  auto pages_of = [&](int b, int& first) {
+    const int from = tokens(a.held, b), to = tokens(a.wanted, b);
+    first = from >> a.page_shift;
+    return to > from ? ((to - 1) >> a.page_shift) + 1 - first : 0;
+  };
+  int mine = 0, skip;
+  for (int b = min(tid * each, a.rows); b < min((tid + 1) * each, a.rows); ++b) mine += pages_of(b, skip);
+  before[tid] = mine;
+  __syncthreads();
+#pragma unroll
+  for (int o = 1; o < NT; o <<= 1) {               // (pages of all rows: below 2^30)
+    const int x = tid >= o ? before[tid - o] : 0;
+    __syncthreads();
+    before[tid] += x;
+    __syncthreads();
+  }
+  const int total = before[NT - 1];
+  const int64_t items = (int64_t)total * a.n_kv_heads;
+  for (int64_t item = (int64_t)blockIdx.x * kBoundWaves + wave; item < items;
+       item += (int64_t)gridDim.x * kBoundWaves) {
+    const int at = (int)(item / a.n_kv_heads), head = (int)(item - (int64_t)at * a.n_kv_heads);
+    // The row: the first thread whose sum passes `at`, then its rows in turn.
+    int lo = 0, hi = NT - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (before[mid] > at) hi = mid;
+      else lo = mid + 1;
+    }
+    int left = at - (lo ? before[lo - 1] : 0), b = lo * each, first, n;
+    while (n = pages_of(b, first), left >= n) left -= n, ++b;
+    const int entry = first + left;
+    const int page = a.table[b * a.table_stride + entry];
+    if (page < 0 || page >= a.n_pages) continue;   // (uniform)
+    const int held = min(tokens(a.wanted, b) - (entry << a.page_shift), 1 << a.page_shift);
+    const char* src = a.k + page * a.page_stride + head * a.head_stride + 16 * (lane % L);
+    float top[N], low[N];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top[i] = -INFINITY, low[i] = INFINITY;
+    constexpr int U = 4;                           // tokens of a lane in flight
+    for (int t = lane / L; t < held; t += U * (64 / L)) {
+      v4u x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)                  // (a token twice does no harm)
+        x[u] = *reinterpret_cast<const v4u*>(src + min(t + u * (64 / L), held - 1) * a.tok_stride);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        T e[N];
+        __builtin_memcpy(e, &x[u], 16);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float v = (float)e[i];
+          bad |= !(fabsf(v) < INFINITY);
+          top[i] = fmaxf(top[i], v);
+          low[i] = fminf(low[i], v);
+        }
+      }
+    }
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int o = L; o < 64; o <<= 1) {
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], o, 64));
+        low[i] = fminf(low[i], __shfl_xor(low[i], o, 64));
+      }
+      most = fmaxf(most, fmaxf(fabsf(top[i]), fabsf(low[i])));
+    }
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    const int e = step_of(most);
+    const bool none = __builtin_amdgcn_ballot_w64(bad) != 0 || e > kHighestStep;
+    const float up = power_of_two(none ? 0 : -e);
+    // The first row of lanes stores the upper bounds, the second the lower ones.
+    if (lane < 2 * L) {
+      const bool upper = lane < L;
+      int8_t code[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        // (a product that falls below the smallest number still rounds away from 0)
+        const float c = upper ? top[i] > 0.f ? fmaxf(ceilf(top[i] * up), 1.f) : ceilf(top[i] * up)
+                              : low[i] < 0.f ? fminf(floorf(low[i] * up), -1.f) : floorf(low[i] * up);
+        code[i] = none ? 0 : (int8_t)c;
+      }
+      const int64_t to = (int64_t)page * a.n_kv_heads + head;
+      __builtin_memcpy(a.codes + to * kBoundBytes + (upper ? 0 : kD) + N * (lane % L), code, N);
+      if (lane == 0) a.scales[to] = none ? INFINITY : power_of_two(e);
+    }
+  }
+}
+
+// --- scores ---------------------------------------------------------------------------------------
+
+// Keys in the order of the scores: 0 for a page that is not there, kAlways for one picked always.
+constexpr uint32_t kAlways = 0xffffffffu;
+__device__ inline uint32_t key_of(float score) {
+  const uint32_t bits = __float_as_uint(score);
+  return bits ^ ((int32_t)bits < 0 ? 0xffffffffu : 0x80000000u);
+}
+
+// Queries of up to 16 heads in 8 bits, as the matrix operand of lane (n, g): head n's channels 16 g ..
+// and 64 + 16 g .. , positive parts and then negative parts.
+struct Say {
+  v4i b[4];
+  int e;                                           // the step's exponent, kNoSay: not finite, or no head
+};
+constexpr int kNoSay = -10000;
+__device__ inline Say say_of(const PagedArgs& p, int64_t at, bool on, int g) {
+  float x[2][16], top = 0.f;
+  bool bad = false;
+  const float sign = p.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    load_queries(p.q, p.q_dtype, at + 64 * u + 16 * g, on, x[u]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      bad |= !(fabsf(x[u][i]) < INFINITY);
+      top = fmaxf(top, fabsf(x[u][i]));
+    }
+  }
+  top = over_groups_max(top);
+  bad = over_groups_max(bad ? 1.f : 0.f) > 0.f;
+  Say s;
+  const int e = step_of(bad ? 0.f : top);
+  s.e = on && !bad ? e : kNoSay;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      uint32_t up = 0u, down = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float c = x[u][4 * d + i] * power_of_two(-e);
+        const int code = bad ? 0 : (int)rintf(sign * c);
+        up |= (uint32_t)(max(code, 0) & 0xff) << 8 * i;
+        down |= (uint32_t)(min(code, 0) & 0xff) << 8 * i;
+      }
+      s.b[u][d] = (int)up;
+      s.b[2 + u][d] = (int)down;
+    }
+  return s;
+}
+
+// A workgroup of four waves scores kChunk pages of a (sequence, KV head), a wave 16 of them at a
+// time.  Reads 260 bytes a page: the memory bounds it, or the launch.  ONE: at most 16 query heads a
+// KV head, in registers; else in LDS.
+constexpr int kChunk = 256;
+
+template <bool ONE>
+__global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
+  constexpr int HG = ONE ? 1 : kMaxSay / 16;
+  __shared__ v4i ops[ONE ? 1 : HG][4][64];
+  __shared__ int exps[HG][16];
+  const PagedArgs& p = a.p;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunks = (p.max_pages + kChunk - 1) / kChunk;
+  const int row = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x % chunks;
+  const int seq = row / p.n_kv_heads, kvh = row % p.n_kv_heads;
+  const int len = min(max(p.seq_len[seq], 0), p.len_max);
+  const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+  if (pages <= a.most || chunk * kChunk >= pages) return;      // (all are picked; none here)
+
+  // The wave's four tiles of pages: entries, then bounds.
+  constexpr int R = kChunk / 64;
+  const int base = chunk * kChunk + wave * 16 * R;
+  int page[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = base + 16 * r + n;
+    page[r] = i < pages ? p.table[seq * p.table_stride + i] : -1;
+    if (page[r] >= p.n_pages) page[r] = -1;
+  }
+  v4i x[R][4];
+  float scale[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t at = (int64_t)max(page[r], 0) * p.n_kv_heads + kvh;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      x[r][s] = *reinterpret_cast<const v4i*>(a.codes + at * kBoundBytes + 64 * s + 16 * g);
+    scale[r] = a.scales[at];
+  }
+
+  const int64_t q_row = seq * p.q_stride + (int64_t)kvh * p.G * kD;
+  Say say;
+  int top_e;
+  if constexpr (ONE) {
+    say = say_of(p, q_row + (int64_t)min(n, p.G - 1) * kD, n < p.G, g);
+    top_e = say.e;
+  } else {
+    top_e = kNoSay;
+    for (int h = wave; h < p.hg; h += 4) {
+      const int head = 16 * h + n;
+      say = say_of(p, q_row + (int64_t)min(head, p.G - 1) * kD, head < p.G, g);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) ops[h][s][lane] = say.b[s];
+      if (g == 0) exps[h][n] = say.e;
+    }
+    __syncthreads();
+    for (int h = 0; h < p.hg; ++h) top_e = max(top_e, exps[h][n]);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top_e = max(top_e, __shfl_xor(top_e, o, 64));
+
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    for (int h = 0; h < (ONE ? 1 : p.hg); ++h) {
+      v4i sum = {0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[r][s], ONE ? say.b[s] : ops[ONE ? 0 : h][s][lane],
+                                                    sum, 0, 0, 0);
+      const int e = ONE ? say.e : exps[ONE ? 0 : h][n];
+      const float w = power_of_two(max(e - top_e, -60));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) best[i] = e == kNoSay ? best[i] : fmaxf(best[i], (float)sum[i] * w);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) best[i] = fmaxf(best[i], __shfl_xor(best[i], o, 64));
+    // Lane (n, g), n < 4, has page 4 g + n of the tile.
+    const float mine = n == 0 ? best[0] : n == 1 ? best[1] : n == 2 ? best[2] : best[3];
+    const int from = (lane & 48) | ((4 * g + n) & 15);
+    const float steps = __shfl(scale[r], from, 64);
+    const bool there = __shfl(page[r], from, 64) >= 0;
+    const int i = base + 16 * r + 4 * g + n;
+    if (n < 4 && i < pages) {
+      const float score = steps == INFINITY ? INFINITY : mine == -INFINITY ? 0.f : mine * steps;
+      const bool always = i < a.first || i >= pages - a.last;
+      a.keys[(int64_t)row * p.max_pages + i] = !there ? 0u : always ? kAlways : key_of(score);
+    }
+  }
+}
+
+// --- the choice, and attention --------------------------------------------------------------------
+
+constexpr int kSparseWaves = 8, kSparseGroups = 256, kSparseCounterStride = 64;
+constexpr size_t kSparseCountersBytes = (size_t)kSparseGroups * kSparseCounterStride * sizeof(unsigned);
+constexpr int kHeldKeys = 16;                      // keys of a thread in registers
+constexpr int kListed = 2048;                      // picked pages of a workgroup in LDS
+
+// A row (a sequence, a KV head, up to 16 of its query heads) has `parts` workgroups.  Each of them finds
+// the row's pages for itself, which takes no longer than to wait for another that does, and attends its
+// share of them with the tile of paged_tile.h; the last one joins the parts.
+template <class M, int QT>
+__global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs a) {
+  constexpr int W = kSparseWaves, NT = 64 * W, TT = M::kTokens, NM = M::kMine;
+  __shared__ JoinSpace<W, kSparseGroups> sh;
+  __shared__ int list_entry[kListed], list_page[kListed];
+  __shared__ int counts[2][W], packed[kHeldKeys * W];
+  __shared__ unsigned arrived;
+  const PagedArgs& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x % a.parts;
+  const int pair = row / p.hg, hgi = row % p.hg;   // (sequence, KV head)
+  const int seq = pair / p.n_kv_heads, kvh = pair % p.n_kv_heads;
+  const int len = min(max(p.seq_len[seq], 0), p.len_max);
+  const int shift = p.page_shift;
+  const int pages = (len + (1 << shift) - 1) >> shift;
+  const int32_t* table = p.table + seq * p.table_stride;
+  const uint32_t* keys = a.keys + (int64_t)pair * p.max_pages;
+  auto exists = [&](int page) { return (page >= 0) & (page < p.n_pages); };
+
+  // Queries early: their loads take as long as the choice.
+  const int heads = min(kPagedHeads, p.G - hgi * kPagedHeads);
+  typename M::template Query<QT> q;
+  q.load(p.q, p.q_dtype,
+         seq * p.q_stride + ((int64_t)kvh * p.G + hgi * kPagedHeads + min(n, heads - 1)) * kD,
+         n < heads, g);
+
+  const bool all = pages <= a.most;                // (then there are no keys)
+  auto key_at = [&](int i) -> uint32_t {
+    return i >= pages ? 0u : all ? (exists(table[i]) ? kAlways : 0u) : keys[i];
+  };
+  uint32_t held[kHeldKeys];
+  const bool fits = pages <= kHeldKeys * NT;
+#pragma unroll
+  for (int r = 0; r < kHeldKeys; ++r) held[r] = r * NT < pages ? key_at(r * NT + tid) : 0u;
+
+  // Pages are picked whose key is above `limit`, and the first `ties` of those with that key.
+  uint32_t limit = 0u;
+  int ties = 0;
+  if (!all) {
+    int turn = 0;
+    auto count = [&](uint32_t least) {             // keys from `least` on
+      int c = 0;
+      if (fits) {
+#pragma unroll
+        for (int r = 0; r < kHeldKeys; ++r)
+          if (r * NT < pages) c += __popcll(__builtin_amdgcn_ballot_w64(held[r] >= least));
+      } else {
+        for (int i = tid; i - tid < pages; i += NT)
+          c += __popcll(__builtin_amdgcn_ballot_w64(key_at(i) >= least));
+      }
+      if (lane == 0) counts[turn & 1][wave] = c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) c += counts[turn & 1][w];
+      ++turn;
+      return __builtin_amdgcn_readfirstlane(c);
+    };
+    if (count(1u) > a.most) {
+      // More than `most` from `lo` on, fewer from `hi` on.
+      uint64_t lo = 1, hi = (uint64_t)1 << 32;
+      int above = 0;
+      while (hi - lo > 1) {
+        const uint64_t mid = (lo + hi) / 2;
+        const int c = count((uint32_t)mid);
+        if (c == a.most) {
+          lo = mid - 1;
+          above = c;
+          break;
+        }
+        if (c > a.most) lo = mid;
+        else hi = mid, above = c;
+      }
+      limit = (uint32_t)lo;
+      ties = a.most - above;
+    }
+  }
+
+  // The picked pages in order: each part keeps its own and those are told.
+  const int first = part * a.run;                  // tiles
+  const int from = (int)((int64_t)first * TT >> shift);
+  const int until = (int)(((int64_t)(first + a.run) * TT + (1 << shift) - 1) >> shift);
+  int gt_before = 0, eq_before = 0;
+  for (int r0 = 0; r0 * NT < pages; r0 += kHeldKeys) {
+    uint64_t gt[kHeldKeys], eq[kHeldKeys];
+    __syncthreads();                               // (`packed` is read)
+#pragma unroll
+    for (int r = 0; r < kHeldKeys; ++r) {
+      gt[r] = eq[r] = 0;
+      if ((r0 + r) * NT < pages) {
+        const uint32_t k = r0 ? key_at((r0 + r) * NT + tid) : held[r];
+        gt[r] = __builtin_amdgcn_ballot_w64(k > limit);
+        eq[r] = ties ? __builtin_amdgcn_ballot_w64(k == limit) : 0;
+      }
+      if (lane == 0) packed[r * W + wave] = __popcll(gt[r]) << 16 | __popcll(eq[r]);
+    }
+    __syncthreads();
+    // Sums before each (r, wave): every wave adds up two entries a lane (fewer than 2^16 of either).
+    static_assert(kHeldKeys * W == 128, "two entries a lane");
+    const int x = packed[2 * lane], y = packed[2 * lane + 1];
+    int incl = x + y;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(incl, o, 64);
+      incl += lane >= o ? up : 0;
+    }
+    const int sums = __builtin_amdgcn_readlane(incl, 63), excl = incl - x - y;
+#pragma unroll
+    for (int r = 0; r < kHeldKeys; ++r) {
+      if ((r0 + r) * NT >= pages) continue;        // (uniform)
+      const int entry = r * W + wave;
+      const int b = __builtin_amdgcn_readlane(excl, entry >> 1) +
+                    (entry & 1 ? __builtin_amdgcn_readlane(x, entry >> 1) : 0);
+      const uint64_t below = ((uint64_t)1 << lane) - 1;
+      const int rank = eq_before + (b & 0xffff) + __popcll(eq[r] & below);
+      const bool tie = (eq[r] >> lane & 1) && rank < ties;
+      const int pos = gt_before + (b >> 16) + __popcll(gt[r] & below) + min(rank, ties);
+      if (((gt[r] >> lane & 1) || tie) && pos >= from && pos < until) {
+        const int i = (r0 + r) * NT + tid;
+        a.picked[(int64_t)pair * a.most + pos] = i;        // (the same by every reader of it)
+        if (pos - from < kListed) {
+          list_entry[pos - from] = i;
+          list_page[pos - from] = table[i];
+        }
+      }
+    }
+    gt_before += sums >> 16;
+    eq_before += sums & 0xffff;
+  }
+  const int picked = gt_before + min(eq_before, ties);
+  const int tiles = (int)(((int64_t)picked << shift) + TT - 1) / TT;
+  const int parts = max(1, (tiles + a.run - 1) / a.run);
+  if (part >= parts) return;                       // (uniform)
+  if (part == 0 && hgi == 0)
+    for (int i = picked + tid; i < a.most; i += NT) a.picked[(int64_t)pair * a.most + i] = -1;
+  __syncthreads();
+
+  // Attention over the picked pages' tokens, as if they were one sequence: token v of it.
+  const int last = min(first + a.run, tiles);
+  struct Place {
+    int page, token;                               // (-1: no page); the first token's index
+  };
+  auto place = [&](int v) {
+    const int j = v >> shift;
+    Place w{-1, 0};
+    if (j < picked) {
+      int entry;
+      if (j - from < kListed) {
+        entry = list_entry[j - from];
+        w.page = list_page[j - from];
+      } else {
+        entry = a.picked[(int64_t)pair * a.most + j];
+        w.page = table[entry];
+      }
+      w.token = (entry << shift) + (v & ((1 << shift) - 1));
+    }
+    return w;
+  };
+  typename M::Keys key;
+  typename M::Values val;
+  auto slot_of = [&](const Place& w) {
+    return kvh * p.head_stride + max(w.page, 0) * p.page_stride +
+           (w.token & ((1 << shift) - 1)) * p.tok_stride;
+  };
+  auto load_keys = [&](int t0) {
+    const int v = t0 + M::key_token(0, n);
+    key.load(p.k + slot_of(place(v)), p.tok_stride, g);
+  };
+  RowPart mine;
+  v4f(&acc)[8] = mine.acc;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+  bool seen = false;
+  Place at{-1, 0};
+  if (first + wave < last) {
+    load_keys((first + wave) * TT);
+    at = place((first + wave) * TT + NM * g);
+    val.load(p.v + slot_of(at), p.tok_stride, n);
+  }
+  for (int i = first + wave; i < last; i += W) {
+    const bool more = i + W < last;
+    float z[NM];
+    M::template scores<QT>(key, q, z);
+    if (more) load_keys((i + W) * TT);
+    const Place next = place(min(i + W, last - 1) * TT + NM * g);
+    if (p.cap > 0.f) {
+      const float in = p.scale / p.cap, back = p.cap * kLog2e;
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] = back * tanh_of(z[e] * in);
+    } else {
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] *= p.scale * kLog2e;
+    }
+    if (__builtin_amdgcn_ballot_w64((at.page < 0) | (at.token + NM > len))) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < NM; ++e) {
+        const bool on = (at.page >= 0) & (at.token + e < len);
+        z[e] = on ? z[e] : -INFINITY;
+        val.keep(e, on);
+        any |= on;
+      }
+      seen |= __builtin_amdgcn_ballot_w64(any) != 0;
+    } else {
+      seen = true;
+    }
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < NM; ++e) m = fmaxf(m, z[e]);
+    m = fmaxf(m_run, over_groups_max(m) - M::kLower);
+    const float ref = m == -INFINITY ? 0.f : m;
+    const float sa = __builtin_amdgcn_exp2f(m_run - ref);      // (0 at the first tile)
+    float w[NM], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < NM; ++e) {
+      w[e] = __builtin_amdgcn_exp2f(z[e] - ref);
+      sum += w[e];
+    }
+    l_run = l_run * sa + sum;
+    m_run = m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] *= sa;
+    M::accumulate(val, w, acc);
+    if (more) val.load(p.v + slot_of(next), p.tok_stride, n);
+    at = next;
+  }
+  mine.m = m_run;
+  mine.l = over_groups_sum(l_run);
+  if (seen && mine.m == -INFINITY && mine.l == 0.f) {          // (NaN scores: the sum is NaN)
+    mine.m = kLowest;
+    mine.l = 1.f;
+  }
+
+  // The waves' parts meet in LDS, the workgroups' in the workspace.
+  if (g == 0) {
+    sh.m[wave][n] = mine.m;
+    sh.l[wave][n] = mine.l;
+  }
+  if (n < heads) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh.sums[wave][n][M::channel(j, i, g)] = acc[j][i];
+  }
+  __syncthreads();
+  const int64_t q_row = (int64_t)seq * p.n_q_heads + kvh * p.G + hgi * kPagedHeads;
+  const auto slots = __builtin_amdgcn_make_buffer_rsrc(p.parts, (short)0, p.parts_bytes, kRsrcWord3);
+  auto finish = [&](int h, int c4, float m, float l, v4f o) {
+    finish_row(p, q_row + h, c4, m, l, o);
+  };
+  auto part_at = [&](int x, int h) {
+    return ((row * a.parts + x) * p.slot_heads + h) * (int)sizeof(Partial);
+  };
+  for (int x = tid; x < heads * (kD / 4); x += NT) {
+    const int h = x / (kD / 4), c4 = x % (kD / 4);
+    float m = sh.m[0][h];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, sh.m[w][h]);
+    float l = 0.f;
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = sh.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[w][h] - m);
+      l += sh.l[w][h] == 0.f ? 0.f : f * sh.l[w][h];
+      o += f * *reinterpret_cast<const v4f*>(&sh.sums[w][h][4 * c4]);
+    }
+    if (parts == 1) {
+      finish(h, c4, m, l, o);
+    } else {
+      const int off = part_at(part, h);
+      __builtin_amdgcn_raw_buffer_store_b128((v4i)o, slots, off + 16 + 16 * c4, 0, kCoherent);
+      if (c4 == 0)
+        __builtin_amdgcn_raw_buffer_store_b128((v4i)(v4f){m, l, 0.f, 0.f}, slots, off, 0, kCoherent);
+    }
+  }
+  if (parts == 1) return;
+  unsigned* counter = p.counters + row * kSparseCounterStride;
+  __builtin_amdgcn_s_waitcnt(0);                   // this thread's stores are done
+  __syncthreads();
+  if (tid == 0)
+    arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (arrived != (unsigned)parts - 1u) return;
+  join_parts(sh, parts, heads, finish, [&](int x, int h, int off) {
+    return (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, part_at(x, h) + off, 0, kCoherent);
+  });
+  if (tid == 0) *counter = 0u;                     // as the next call expects it
+}
+
+// Rows, and part slots: rows that are shared are so by no more workgroups than fill the chip.
+int64_t sparse_rows(int64_t batch, int n_q_heads, int n_kv_heads) {
+  const int G = n_q_heads / n_kv_heads;
+  return batch * n_kv_heads * ((G + kPagedHeads - 1) / kPagedHeads);
+}
+size_t sparse_parts_bytes(int slot_heads) {
+  return (size_t)kSparseGroups * slot_heads * sizeof(Partial);
+}
+int slot_heads_of(int n_q_heads, int n_kv_heads) {
+  return std::min(n_q_heads / n_kv_heads, kPagedHeads);
+}
+
+}  // namespace
+
+aatc_status launch_bounds(const BoundsArgs& a, aatc_dtype dtype, void* stream) {
+  const int64_t items = (int64_t)a.rows * a.max_pages * a.n_kv_heads;
+  const int64_t grid = std::min<int64_t>(kBoundGroups, (items + kBoundWaves - 1) / kBoundWaves);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kBoundWaves), 0, (hipStream_t)stream,
+                       a);
+    return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
+  };
+  switch (dtype) {
+    case AATC_F32: return launch(bounds_kernel<float>);
+    case AATC_BF16: return launch(bounds_kernel<__bf16>);
+    default: return launch(bounds_kernel<_Float16>);
+  }
+}
+
+size_t sparse_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int64_t max_pages) {
+  return kSparseCountersBytes + round256(sparse_parts_bytes(slot_heads_of(n_q_heads, n_kv_heads))) +
+         (size_t)batch * n_kv_heads * max_pages * sizeof(uint32_t);
+}
+
+bool sparse_fits(int64_t batch, int n_q_heads, int n_kv_heads, int64_t max_pages) {
+  if (n_q_heads / n_kv_heads > kMaxSay) return false;
+  const int64_t pairs = batch * n_kv_heads;
+  if (max_pages > ((int64_t)1 << 30) / pairs) return false;
+  return pairs * ((max_pages + kChunk - 1) / kChunk) <= kMaxSparseGroups &&
+         sparse_rows(batch, n_q_heads, n_kv_heads) <= kMaxSparseGroups;
+}
+
+aatc_status launch_sparse(SparseArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
+  PagedArgs& p = a.p;
+  p.slot_heads = slot_heads_of(p.n_q_heads, p.n_kv_heads);
+  p.len_max = std::min(p.len_max, INT32_MAX - 16384);          // (tokens of whole tiles: 32 bits)
+  p.counters = static_cast<unsigned*>(workspace);
+  char* parts = static_cast<char*>(workspace) + kSparseCountersBytes;
+  p.parts = reinterpret_cast<Partial*>(parts);
+  p.parts_bytes = (int)sparse_parts_bytes(p.slot_heads);
+  a.keys = reinterpret_cast<uint32_t*>(parts + round256(p.parts_bytes));
+  const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
+  const int64_t rows = sparse_rows(p.batch, p.n_q_heads, p.n_kv_heads);
+  const int64_t tokens = (int64_t)std::min(a.most, p.max_pages) << p.page_shift;
+  const int tiles = (int)((tokens + tt - 1) / tt);
+  // Rows are shared where there are fewer than workgroups, two tiles a wave at least.
+  const int share = rows < kSparseGroups ? kSparseGroups / (int)rows : 1;
+  a.run = std::max((tiles + share - 1) / share, std::min(tiles, 2 * kSparseWaves));
+  a.parts = (tiles + a.run - 1) / a.run;
+  const hipStream_t st = (hipStream_t)stream;
+  if (p.max_pages > a.most) {                      // (else every page is picked)
+    const int64_t groups = (int64_t)p.batch * p.n_kv_heads * ((p.max_pages + kChunk - 1) / kChunk);
+    if (p.hg == 1)
+      hipLaunchKernelGGL(score_kernel<true>, dim3((unsigned)groups), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(score_kernel<false>, dim3((unsigned)groups), dim3(256), 0, st, a);
+    if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
+  }
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * a.parts)), dim3(64 * kSparseWaves), 0, st, a);
+    return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
+  };
+  using One = std::integral_constant<int, 1>;
+  using Three = std::integral_constant<int, 3>;
+  const bool same = p.q_dtype == (int)c_dtype;
+  auto launch_as = [&](auto m, auto qt) {
+    return launch(sparse_kernel<decltype(m), decltype(qt)::value>);
+  };
+  switch (c_dtype) {
+    case AATC_F32: return launch_as(Full32<false>{}, One{});
+    case AATC_BF16:
+      return same ? launch_as(Half16<__bf16, false>{}, One{})
+                  : launch_as(Half16<__bf16, false>{}, Three{});
+    default:
+      return same ? launch_as(Half16<_Float16, false>{}, One{})
+                  : launch_as(Half16<_Float16, false>{}, Three{});
+  }
+}
+
+}  // namespace aatc
