@@ -45,9 +45,8 @@ extern "C" {
  * out       device [batch][max_draft][n_q_heads][d] fp32, 16-byte aligned; drafts from n_draft[b] on
  *           are left as they were (here and in lse).
  * lse       device [batch][max_draft][n_q_heads] fp32 or NULL.
- * workspace device scratch of aatc_paged_tree_workspace_bytes bytes, 256-byte aligned, zero-filled
- *           once after allocation; every call leaves it reusable, for calls of other shapes that it is
- *           large enough for too.  Calls that may overlap need one each.
+ * workspace device scratch of aatc_paged_tree_workspace_bytes bytes, 256-byte aligned, of any content.
+ *           Calls that may overlap need one each.
  * Other arguments as in aatc_paged_decode_attention.
  * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; max_draft; more than 2^30 tiles of 16 tokens;
  * max_draft * n_q_heads / n_kv_heads over 16384), AATC_E_WORKSPACE, AATC_E_DEVICE.

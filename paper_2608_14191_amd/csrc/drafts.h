@@ -20,6 +20,7 @@ struct TreeArgs {
   int drafts;                     // of each sequence at most
   int blocks, block_cols;         // a (sequence, KV head)'s queries: blocks of so many columns
   int units;                      // runs of tokens that fill the chip (each `blocks` workgroups)
+  int quantum;                    // tiles
 };
 
 size_t tree_workspace_bytes(int batch, int drafts, int n_q_heads, int n_kv_heads);

@@ -5,13 +5,14 @@
 // head j of draft i.  For column c over its attended tokens t
 //   z_t = cap tanh(scale q_c . k_t / cap) - slope (pos_c - pos_t),   o_c = sum_t softmax(z)_t v_t.
 //
-// One pass with a running maximum and sum, on the tile of paged_tile.h: a wave takes 32 tokens (16 in
-// float32) against up to C groups of 16 columns, so that keys and values are read once for all of
-// them and values are turned once.  The queries of C > 1 groups lie in LDS as matrix operands.
-//
-// What bounds it: few columns (m G <= 16) the memory, as one token does; 64 columns and more the
-// matrix cores (P in two or three terms: 1.5 or 2 products for one of a plain attention) and the
-// vector units (exponentials, splitting) about alike.
+// One pass with a running maximum and sum, on the tile of paged_tile.h: 32 tokens (16 in float32)
+// against groups of 16 columns.  Two kernels:
+//   up to 16 columns, bound by the memory as one token's attention is: every wave takes tiles for
+//   itself, keys and values go from memory to its registers;
+//   more, bound by the matrix cores (P in two or three terms: 1.5 or 2 products for one of a plain
+//   attention) and the vector units (exponentials, splitting) about alike: the waves of a workgroup
+//   share the tiles of a stage in LDS, each with up to 48 of its columns, so that a compute unit reads
+//   keys and values once for up to 256 columns.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,46 +26,34 @@
 namespace aatc {
 namespace {
 
-// Eight waves a workgroup, one workgroup a compute unit: a row has few parts to join.
-constexpr int kTreeWaves = 8, kTreeGroups = 256;
+// One workgroup a compute unit, so that a row has few parts to join.
+constexpr int kTreeGroups = 256;
 constexpr int kGroup = 16;                        // columns of a group
-constexpr int kMostGroups = 4;                    // of a workgroup
-// The workspace: arrival counters of the rows that are shared (256 bytes apart, left at zero), then
-// part slots.  At most twice as many runs as fill the chip belong to shared rows.
-constexpr int kTreeSlots = 2 * kTreeGroups, kTreeCounterStride = 64;
-constexpr size_t kTreeCountersBytes = (size_t)kTreeSlots * kTreeCounterStride * sizeof(unsigned);
-// (column, part) pairs of a joined block: their weights are kept in LDS.
-constexpr int kMostPairs = 8192;
+constexpr int kMostCols = 256;                    // of a workgroup
+// The workspace: part slots.  At most twice as many runs as fill the chip belong to shared rows.
+constexpr int kTreeSlots = 2 * kTreeGroups;
+// Runs are a multiple of so many tiles, twice that at least: a tile a wave for the narrow kernel, a
+// stage for the wide one.
+constexpr int kNarrowQuantum = 8, kWideQuantum = 2;
 // The maximum that weights refer to is renewed when a score passes it by this much (exponents of 2):
-// sums and outputs are rescaled rarely.  Weights of 2^(slack + lower) have to fit their type.
+// sums and outputs are rescaled rarely.  Weights of 2^(slack + below) have to fit their type, and in
+// f16 small ones stay off the denormals.
 template <class M>
 constexpr float kSlack = std::is_same_v<typename M::Elem, _Float16> ? 6.f : 8.f;
 template <class M>
 constexpr float kBelow = std::is_same_v<typename M::Elem, _Float16> ? 9.f : 0.f;
 
+// The window that the shallowest and the deepest of m drafts have together.
 __host__ __device__ inline int window_of(int window, int m) {
   return window > 0 ? min(window, 1 << 30) + m - 1 : 0;
 }
 
-template <class M, int QT, int C>
-struct TreeSpace {
-  using Query = typename M::template Query<QT>;
-  static constexpr int kPieces = sizeof(Query::t) / 16;
-  union {
-    v4u q[C][kPieces][64];
-    float sums[kTreeWaves][kGroup][kD + 4];        // (rows padded: banks)
-    struct {
-      float m[kMostPairs], l[kMostPairs];
-    } parts;
-  };
-  float back[C][kGroup], slope[C][kGroup];
-  int draft[C][kGroup];
+// Who the columns of a workgroup are, and who descends from whom (LDS).
+struct TreeInfo {
   uint64_t family[kMaxDrafts];                     // a draft and its ancestors
   int depth[kMaxDrafts];
-  float m[kTreeWaves][kGroup], l[kTreeWaves][kGroup];
-  float top[C * kGroup], total[C * kGroup];
-  int scan[2][kTreeWaves], found[4];
-  unsigned arrived;
+  int draft[kMostCols];
+  float slope[kMostCols];
 };
 
 // This thread's number plus those of the threads before it; `total`: of all.
@@ -91,275 +80,291 @@ __device__ inline int scan_all(int x, int* space, int& total) {
   return incl;
 }
 
-template <class M, int QT, int C>
-__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeArgs a) {
-  constexpr int W = kTreeWaves, NT = 64 * W, TT = M::kTokens, NM = M::kMine;
-  using Space = TreeSpace<M, QT, C>;
-  using Query = typename Space::Query;
-  constexpr int NF = Space::kPieces;
-  constexpr bool kHasBack = sizeof(Query) != sizeof(Query::t);
-  __shared__ Space sh;
-  const PagedArgs& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int heads = p.n_kv_heads;
-  // The column blocks of one run read the same tokens: they are on one XCD (workgroups go to the
-  // eight in turn) at one time, and meet in its L2.
-  const int block = (int)blockIdx.x;
-  const int unit = (block >> 3) / a.blocks * 8 + (block & 7), cb = (block >> 3) % a.blocks;
-  const auto slots = __builtin_amdgcn_make_buffer_rsrc(p.parts, (short)0, p.parts_bytes, kRsrcWord3);
+__device__ inline int cached_of(const TreeArgs& a, int b) {
+  return min(max(a.p.seq_len[b], 0), a.p.len_max);
+}
+__device__ inline int drafts_of(const TreeArgs& a, int b) {
+  return a.n_draft ? min(max(a.n_draft[b], 0), a.drafts) : a.drafts;
+}
 
-  auto cached = [&](int b) { return min(max(p.seq_len[b], 0), p.len_max); };
-  auto drafted = [&](int b) {
-    return a.n_draft ? min(max(a.n_draft[b], 0), a.drafts) : a.drafts;
-  };
-  auto tiles_of = [&](int b) {
-    const int m = drafted(b);
-    return row_tiles(cached(b) + m, window_of(p.window, m), p.sink, TT);
-  };
-
-  // The runs: every row (a sequence and KV head, all columns) in runs of at most `most` tiles.
-  const int each = (p.batch + NT - 1) / NT;
-  const int b0 = min(tid * each, p.batch), b1 = min(b0 + each, p.batch);
-  int seq = 0, runs_before = 0, shared_before = 0, most;
+// The runs: every row (a sequence and KV head, all columns) in runs of nearly equal length, the runs
+// of all rows in one list.
+struct TreeRun {
+  int seq, kvh, part, parts;
+  int first, last;                                 // tiles
+  int shared;                                      // the row's first part slot (part q's: heads q further)
+  int len, m;                                      // tokens, drafts
   RowTiles rt;
-  const int cap_parts = kMostPairs / a.block_cols;
+};
+
+// Run `unit` of the list; false: there is none (for all threads alike).
+template <int TT, int W>
+__device__ inline bool find_run(const TreeArgs& a, int unit, int (*scan)[W], int* found, TreeRun& r) {
+  constexpr int NT = 64 * W;
+  const PagedArgs& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, heads = p.n_kv_heads;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto tiles_of = [&](int b) {
+    const int m = drafts_of(a, b);
+    return row_tiles(cached_of(a, b) + m, window_of(p.window, m), p.sink, TT);
+  };
+  int before = 0, shared = 0, most;
+  r.seq = 0;
   if (p.batch == 1) {
-    if (drafted(0) == 0) return;                   // (uniform)
-    rt = tiles_of(0);
-    most = W * smallest_rounds(rt.n * heads, rt.n, heads, a.units, W,
-                               [&](int q) { return heads * runs_of(rt.n, q); });
-    most = max(most, runs_of(rt.n, cap_parts));
+    if (drafts_of(a, 0) == 0) return false;
+    r.rt = tiles_of(0);
+    most = a.quantum * smallest_rounds(r.rt.n * heads, r.rt.n, heads, a.units, a.quantum,
+                                       [&](int q) { return heads * runs_of(r.rt.n, q); });
   } else {
+    const int each = (p.batch + NT - 1) / NT;
+    const int b0 = min(tid * each, p.batch), b1 = min(b0 + each, p.batch);
     int mine = 0, longest = 0, rows = 0, tiles;
     for (int b = b0; b < b1; ++b) {
-      const int t = drafted(b) ? tiles_of(b).n : 0;
+      const int t = drafts_of(a, b) ? tiles_of(b).n : 0;
       mine += t;
       rows += t > 0;
       longest = max(longest, t);
     }
-    scan_all<W>(mine, sh.scan[0], tiles);
-    scan_all<W>(rows, sh.scan[1], rows);
+    scan_all<W>(mine, scan[0], tiles);
+    scan_all<W>(rows, scan[1], rows);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) longest = max(longest, __shfl_xor(longest, o, 64));
     __syncthreads();
-    if (lane == 0) sh.scan[0][wave] = longest;
+    if (lane == 0) scan[0][wave] = longest;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < W; ++w) longest = max(longest, sh.scan[0][w]);
+    for (int w = 0; w < W; ++w) longest = max(longest, scan[0][w]);
     longest = __builtin_amdgcn_readfirstlane(longest);
-    if (tiles == 0) return;                        // (uniform)
+    if (tiles == 0) return false;
     auto runs = [&](int q) {
-      int r = 0, all;
-      for (int b = b0; b < b1; ++b) r += drafted(b) ? runs_of(tiles_of(b).n, q) : 0;
-      scan_all<W>(r, sh.scan[0], all);
+      int n = 0, all;
+      for (int b = b0; b < b1; ++b) n += drafts_of(a, b) ? runs_of(tiles_of(b).n, q) : 0;
+      scan_all<W>(n, scan[0], all);
       return heads * all;
     };
+    // Rows that fit the chip are cut into runs that do; more rows into runs as long as the average
+    // share: no more than `units` of them beyond one a row.
     if (rows * heads <= a.units)
-      most = W * smallest_rounds(tiles * heads, longest, rows * heads, a.units, W, runs);
+      most = a.quantum * smallest_rounds(tiles * heads, longest, rows * heads, a.units, a.quantum, runs);
     else
-      most = max((int)(((int64_t)tiles * heads + a.units - 1) / a.units), kRoundsMin * W);
-    most = max(most, runs_of(longest, cap_parts));
+      most = max((int)(((int64_t)tiles * heads + a.units - 1) / a.units), kRoundsMin * a.quantum);
     // Which sequence has this run, and the runs and the shared rows' runs before it.
-    int r = 0, s = 0, total;
+    int n = 0, s = 0, total, spare;
     for (int b = b0; b < b1; ++b) {
-      const int k = drafted(b) ? runs_of(tiles_of(b).n, most) : 0;
-      r += heads * k;
+      const int k = drafts_of(a, b) ? runs_of(tiles_of(b).n, most) : 0;
+      n += heads * k;
       s += k > 1 ? heads * k : 0;
     }
-    const int incl = scan_all<W>(r, sh.scan[0], total);
-    int spare, at_shared = scan_all<W>(s, sh.scan[1], spare) - s;
-    if (unit >= total) return;                     // (uniform)
-    int at = incl - r;
+    const int incl = scan_all<W>(n, scan[0], total);
+    int at_shared = scan_all<W>(s, scan[1], spare) - s;
+    if (unit >= total) return false;
+    int at = incl - n;
     if (unit >= at && unit < incl) {               // (one thread)
       int b = b0;
       for (;; ++b) {
-        const int k = drafted(b) ? runs_of(tiles_of(b).n, most) : 0;
+        const int k = drafts_of(a, b) ? runs_of(tiles_of(b).n, most) : 0;
         if (unit < at + heads * k) break;
         at += heads * k;
         at_shared += k > 1 ? heads * k : 0;
       }
-      sh.found[0] = b;
-      sh.found[1] = at;
-      sh.found[2] = at_shared;
+      found[0] = b;
+      found[1] = at;
+      found[2] = at_shared;
     }
     __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(sh.found[0]);
-    runs_before = __builtin_amdgcn_readfirstlane(sh.found[1]);
-    shared_before = __builtin_amdgcn_readfirstlane(sh.found[2]);
-    rt = tiles_of(seq);
+    r.seq = __builtin_amdgcn_readfirstlane(found[0]);
+    before = __builtin_amdgcn_readfirstlane(found[1]);
+    shared = __builtin_amdgcn_readfirstlane(found[2]);
+    r.rt = tiles_of(r.seq);
   }
-  const int parts = runs_of(rt.n, most);
-  const int kvh = (unit - runs_before) % heads, part = (unit - runs_before) / heads;
-  const int len = cached(seq), m = drafted(seq), G = p.G;
-  const int columns = min(m * G - cb * a.block_cols, a.block_cols);
-  if (part >= parts || columns <= 0) return;       // (uniform)
-  const int groups = (columns + kGroup - 1) / kGroup;
-  const int first = run_begin(rt.n, parts, part), last = run_begin(rt.n, parts, part + 1);
-  const int end = len + m;
-  const int lo = p.window > 0 ? max(0, end - window_of(p.window, m)) : 0;
+  r.parts = runs_of(r.rt.n, most);
+  r.kvh = (unit - before) % heads;
+  r.part = (unit - before) / heads;
+  if (r.part >= r.parts) return false;
+  r.shared = shared + r.kvh;
+  r.len = cached_of(a, r.seq);
+  r.m = drafts_of(a, r.seq);
+  r.first = run_begin(r.rt.n, r.parts, r.part);
+  r.last = run_begin(r.rt.n, r.parts, r.part + 1);
+  return true;
+}
 
-  // Queries, and who descends from whom.
-  Query own;
-  auto column = [&](int c) { return cb * a.block_cols + c * kGroup + n; };
-  auto fetch_query = [&](int c, Query& q) {
-    const bool on = c * kGroup + n < columns;
-    const int x = on ? column(c) : cb * a.block_cols, i = x / G, j = x - i * G;
-    q.load(p.q, p.q_dtype,
-           ((int64_t)seq * a.drafts + i) * p.q_stride + (int64_t)(kvh * G + j) * kD, on, g);
-    if (g == 0) {
-      sh.draft[c][n] = i;
-      sh.slope[c][n] = p.slopes && on ? p.slopes[kvh * G + j] * kLog2e : 0.f;
-    }
-  };
-  if constexpr (C == 1) {
-    fetch_query(0, own);                           // (every wave its own registers)
-  } else if (wave < groups) {
-    fetch_query(wave, own);
-    v4u piece[NF];
-    __builtin_memcpy(piece, &own.t, sizeof own.t);
+// Families and depths of a sequence's drafts (one wave, a lane a draft).
+__device__ inline void find_families(const TreeArgs& a, const TreeRun& r, TreeInfo& info) {
+  const int lane = threadIdx.x & 63;
+  int up = lane < r.m ? (a.parent ? a.parent[(int64_t)r.seq * a.drafts + lane] : lane - 1) : -1;
+  up = up < lane ? max(up, -1) : -1;
+  uint64_t family = (uint64_t)1 << lane;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) sh.q[wave][f][lane] = piece[f];
-    if constexpr (kHasBack) {
-      if (g == 0) sh.back[wave][n] = own.back;
-    }
+  for (int d = 1; d < kMaxDrafts; d <<= 1) {       // ancestors up to 2 d - 1 steps away
+    const int from = max(up, 0);
+    const uint64_t theirs = __shfl(family, from, 64);
+    const int higher = __shfl(up, from, 64);
+    family |= up >= 0 ? theirs : 0;
+    up = up >= 0 ? higher : -1;
   }
-  if (wave == W - 1) {
-    int up = lane < m ? (a.parent ? a.parent[(int64_t)seq * a.drafts + lane] : lane - 1) : -1;
-    up = up < lane ? max(up, -1) : -1;
-    uint64_t family = (uint64_t)1 << lane;
-#pragma unroll
-    for (int d = 1; d < kMaxDrafts; d <<= 1) {     // ancestors up to 2 d - 1 steps away
-      const int from = max(up, 0);
-      const uint64_t theirs = __shfl(family, from, 64);
-      const int higher = __shfl(up, from, 64);
-      family |= up >= 0 ? theirs : 0;
-      up = up >= 0 ? higher : -1;
-    }
-    sh.family[lane] = family;
-    sh.depth[lane] = __popcll(family) - 1;
-  }
+  info.family[lane] = family;
+  info.depth[lane] = __popcll(family) - 1;
+}
 
-  // Pages, keys and values.
-  typename M::Keys key;
-  typename M::Values val;
-  const int32_t* row = p.table + seq * p.table_stride;
-  auto page_of = [&](int t) {
+// Where the tokens of a sequence and KV head lie.
+struct TreePages {
+  const PagedArgs& p;
+  const int32_t* row;
+  int64_t head;
+  __device__ TreePages(const PagedArgs& args, int seq, int kvh)
+      : p(args), row(args.table + seq * args.table_stride), head(kvh * args.head_stride) {}
+  __device__ int page_of(int t) const {
     const int i = t >> p.page_shift;
     return i < p.max_pages ? row[i] : -1;
-  };
-  auto exists = [&](int page) { return (page >= 0) & (page < p.n_pages); };
-  auto slot_of = [&](int t, int page) {
-    return kvh * p.head_stride + (exists(page) ? page : 0) * p.page_stride +
+  }
+  __device__ bool exists(int page) const { return (page >= 0) & (page < p.n_pages); }
+  __device__ int64_t slot_of(int t, int page) const {
+    return head + (exists(page) ? page : 0) * p.page_stride +
            (t & ((1 << p.page_shift) - 1)) * p.tok_stride;
-  };
-  auto load_keys = [&](int t0, int page) {
-    key.load(p.k + slot_of(t0 + M::key_token(0, n), page), p.tok_stride, g);
-  };
-  auto load_values = [&](int t0, int page) {
-    val.load(p.v + slot_of(t0 + NM * g, page), p.tok_stride, n);
-  };
-  auto key_page = [&](int t0) { return page_of(t0 + 8 * M::key_block(n)); };
-  auto value_page = [&](int t0) { return page_of(t0 + 8 * M::value_block(g)); };
-  const int begin = first + wave;
-  int t0 = rt.token(min(begin, last - 1), TT), t1 = rt.token(min(begin + W, last - 1), TT);
-  int vp = value_page(t0), kp1 = key_page(t1), vp1 = value_page(t1);
-  if (begin < last) {
-    load_keys(t0, key_page(t0));
-    load_values(t0, vp);
   }
-  __syncthreads();
+};
 
+// What a wave has of C groups of columns, from column col0 of the workgroup's block on: running
+// maxima (exponents of 2), sums and value sums (acc[c][j][i]: channel M::channel(j, i, g) of column
+// 16 c + n).
+template <class M, int QT, int C>
+struct TreeWave {
+  using Tile = M;
+  static constexpr int TT = M::kTokens, NM = M::kMine;
+  const PagedArgs& p;
+  const TreeInfo& info;
+  const int n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  int col0, len, end, lo;
+  typename M::template Query<QT> q[C];
   v4f acc[C][8];
-  float m_run[C], l_run[C], back[C];
+  float m_run[C], l_run[C];
   unsigned seen = 0u;                              // bit c: any token attended by the lane's column
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    m_run[c] = -INFINITY;
-    l_run[c] = 0.f;
-    back[c] = 1.f;
-    if constexpr (C > 1 && kHasBack) back[c] = sh.back[c][n];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[c][j] = (v4f){0.f, 0.f, 0.f, 0.f};
-  }
-  for (int i = begin; i < last; i += W) {
-    const bool more = i + W < last;
-    float z[C][NM];
-    // (the queries are read here each time: they have no room in registers)
-    if constexpr (C > 1) asm volatile("" ::: "memory");
+  bool odd = false;                                // values that are not finite in a masked tile
+
+  __device__ TreeWave(const TreeArgs& a, const TreeRun& r, TreeInfo& space, int block, int first,
+                      int columns)
+      : p(a.p), info(space), col0(first), len(r.len), end(r.len + r.m) {
+    lo = p.window > 0 ? max(0, end - window_of(p.window, r.m)) : 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (c >= groups) continue;                   // (uniform)
-      if constexpr (C == 1) {
-        M::template scores<QT>(key, own, z[c]);
-      } else {
-        Query q;
-        v4u piece[NF];
-#pragma unroll
-        for (int f = 0; f < NF; ++f) piece[f] = sh.q[c][f][lane];
-        __builtin_memcpy(&q.t, piece, sizeof q.t);
-        if constexpr (kHasBack) q.back = back[c];
-        M::template scores<QT>(key, q, z[c]);
+      const int col = first + c * kGroup + n;
+      const bool on = col < columns;
+      const int x = block * a.block_cols + (on ? col : 0), i = x / p.G, j = x - i * p.G;
+      q[c].load(p.q, p.q_dtype,
+                ((int64_t)r.seq * a.drafts + i) * p.q_stride + (int64_t)(r.kvh * p.G + j) * kD, on, g);
+      if (g == 0) {                                // (waves with the same columns write the same)
+        space.draft[col] = i;
+        space.slope[col] = p.slopes && on ? p.slopes[r.kvh * p.G + j] * kLog2e : 0.f;
       }
+      m_run[c] = -INFINITY;
+      l_run[c] = 0.f;
+#pragma unroll
+      for (int j8 = 0; j8 < 8; ++j8) acc[c][j8] = (v4f){0.f, 0.f, 0.f, 0.f};
     }
-    if (more) load_keys(t1, kp1);
-    const int t2 = rt.token(min(i + 2 * W, last - 1), TT);
-    const int kp2 = key_page(t2), vp2 = value_page(t2);
-    // A tile that all columns attend as a whole needs no masks: the deepest draft stands at most
-    // at end - 1.
-    const bool there = exists(vp);
-    const bool whole = t0 + TT <= len && (p.window == 0 || t0 > end - 1 - p.window || t0 + TT <= p.sink) &&
-                       __builtin_amdgcn_ballot_w64(!there) == 0;
-    unsigned dirty = 0u;                           // bit e: token NM g + e of the tile
-    if (!whole) {
+  }
+
+  // A tile that all columns attend as a whole needs no masks: the deepest draft stands at most at
+  // end - 1.  `there`: whether the lane's values' page is.
+  __device__ bool is_whole(int t0, bool there) const {
+    return t0 + TT <= len &&
+           (p.window == 0 || t0 > end - 1 - p.window || t0 + TT <= p.sink) &&
+           __builtin_amdgcn_ballot_w64(!there) == 0;
+  }
+
+  // Tokens that no column attends become zeros; returns which others are not finite (bit e).
+  __device__ unsigned mask_values(int t0, bool there, typename M::Values& val) const {
+#pragma unroll
+    for (int e = 0; e < NM; ++e) {
+      const int t = t0 + NM * g + e;
+      val.keep(e, there & (t < end) & ((t >= lo) | (t < p.sink)));
+    }
+    unsigned dirty = 0u;
+    if (__builtin_amdgcn_ballot_w64(M::any_bad(val)))
+#pragma unroll
+      for (int e = 0; e < NM; ++e)
+        dirty |= __builtin_amdgcn_ballot_w64(M::bad(val, e)) >> (16 * g) & 0xffffu ? 1u << e : 0u;
+    return dirty;
+  }
+
+  // Scores as exponents of 2, -infinity where a column does not attend; returns where it does (bit e).
+  __device__ unsigned weigh(int c, int t0, bool whole, bool there, float (&z)[NM]) const {
+    unsigned bits = ~0u;
+    if (p.cap > 0.f) {
+      const float in = p.scale / p.cap, out = p.cap * kLog2e;
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] = out * tanh_of(z[e] * in);
+    } else {
+#pragma unroll
+      for (int e = 0; e < NM; ++e) z[e] *= p.scale * kLog2e;
+    }
+    if (p.slopes || !whole) {
+      const int col = col0 + c * kGroup + n;
+      const int draft = info.draft[col], pos = len + info.depth[draft];
+      const uint64_t family = info.family[draft];
+      const float slope = info.slope[col];
+      if (!whole) bits = 0u;
 #pragma unroll
       for (int e = 0; e < NM; ++e) {
-        val.keep(e, there & (t0 + NM * g + e < end) &
-                        ((t0 + NM * g + e >= lo) | (t0 + NM * g + e < p.sink)));
-        dirty |= M::bad(val, e) ? 1u << e : 0u;
-      }
-    }
-    unsigned on_bits[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      on_bits[c] = ~0u;
-      if (c >= groups) continue;                   // (uniform)
-      if (p.cap > 0.f) {
-        const float in = p.scale / p.cap, out = p.cap * kLog2e;
-#pragma unroll
-        for (int e = 0; e < NM; ++e) z[c][e] = out * tanh_of(z[c][e] * in);
-      } else {
-#pragma unroll
-        for (int e = 0; e < NM; ++e) z[c][e] *= p.scale * kLog2e;
-      }
-      if (p.slopes || !whole) {
-        const int draft = sh.draft[c][n], pos = len + sh.depth[draft];
-        const uint64_t family = sh.family[draft];
-        const float slope = sh.slope[c][n];
-        if (!whole) on_bits[c] = 0u;
-#pragma unroll
-        for (int e = 0; e < NM; ++e) {
-          const int t = t0 + NM * g + e;
-          const int j = min(max(t - len, 0), kMaxDrafts - 1);
-          const int at = whole || t < len ? t : len + sh.depth[j];
-          if (p.slopes) z[c][e] -= slope * (float)(pos - at);
-          if (!whole) {
-            // (no short circuits: selects, not branches)
-            const bool kin = (t < len) | ((t < end) & (bool)(family >> j & 1));
-            const bool near = (p.window == 0) | (pos - at < p.window) | (t < p.sink);
-            const bool on = there & kin & near;
-            z[c][e] = on ? z[c][e] : -INFINITY;
-            on_bits[c] |= on ? 1u << e : 0u;
-          }
+        const int t = t0 + NM * g + e;
+        const int j = min(max(t - len, 0), kMaxDrafts - 1);
+        const int at = whole || t < len ? t : len + info.depth[j];
+        if (p.slopes) z[e] -= slope * (float)(pos - at);
+        if (!whole) {
+          // (no short circuits: selects, not branches)
+          const bool kin = (t < len) | ((t < end) & (bool)(family >> j & 1));
+          const bool near = (p.window == 0) | (pos - at < p.window) | (t < p.sink);
+          const bool on = there & kin & near;
+          z[e] = on ? z[e] : -INFINITY;
+          bits |= on ? 1u << e : 0u;
         }
       }
-      seen |= on_bits[c] ? 1u << c : 0u;
-      float top = z[c][0];
+    }
+    return bits;
+  }
+
+  // One tile.  next_values and next_keys: called when the registers are free for the next ones.
+  template <class V, class K>
+  __device__ void step(int t0, bool there, const typename M::Keys& key, typename M::Values& val,
+                       V next_values, K next_keys) {
+    const bool whole = is_whole(t0, there);
+    if (!whole) {
+      const unsigned dirty = mask_values(t0, there, val);
+      if (__builtin_amdgcn_ballot_w64(dirty != 0u)) {
+        odd = true;                                // (these tokens: odd_values)
 #pragma unroll
-      for (int e = 1; e < NM; ++e) top = fmaxf(top, z[c][e]);
-      top = over_groups_max(top) - kBelow<M>;
-      if (__builtin_amdgcn_ballot_w64(top > m_run[c] + kSlack<M>)) {
-        const float next = top > m_run[c] + kSlack<M> ? top : m_run[c];
+        for (int e = 0; e < NM; ++e) val.keep(e, !(dirty >> e & 1u));
+      }
+    }
+    typename M::Turned turned;
+    M::turn(val, turned);
+    next_values();
+    float z[C][NM];
+#pragma unroll
+    for (int c = 0; c < C; ++c) M::template scores<QT>(key, q[c], z[c]);
+    next_keys();
+    float unit = p.scale * kLog2e;                 // (scores that are only scaled are so on the way)
+    if (whole && p.cap == 0.f && !p.slopes && p.scale > 0.f) {
+      seen = ~0u;
+    } else {
+      unit = 1.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) seen |= weigh(c, t0, whole, there, z[c]) ? 1u << c : 0u;
+    }
+    float top[C];
+    bool higher = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      top[c] = z[c][0];
+#pragma unroll
+      for (int e = 1; e < NM; ++e) top[c] = fmaxf(top[c], z[c][e]);
+      higher |= top[c] * unit - kBelow<M> > m_run[c] + kSlack<M>;
+    }
+    if (__builtin_amdgcn_ballot_w64(higher)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float most = over_groups_max(top[c]) * unit - kBelow<M>;
+        const float next = most > m_run[c] + kSlack<M> ? most : m_run[c];
         const float ref = next == -INFINITY ? 0.f : next;
         const float sa = __builtin_amdgcn_exp2f(m_run[c] - ref);    // (0 at the first tile)
         l_run[c] *= sa;
@@ -367,257 +372,528 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] *= sa;
       }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
       const float ref = m_run[c] == -INFINITY ? 0.f : m_run[c];
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < NM; ++e) {
-        z[c][e] = __builtin_amdgcn_exp2f(z[c][e] - ref);
+        z[c][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[c][e], unit, -ref));
         sum += z[c][e];
       }
       l_run[c] += sum;
-    }
-    // Values that are not finite count for the columns that attend them and for no others (0 times
-    // them is NaN): such tokens, if there are any, one by one, with a choice behind the product.
-    if (__builtin_amdgcn_ballot_w64(dirty != 0u)) {
-      for (int tok = 0; tok < TT; ++tok) {
-        const int ge = tok / NM, te = tok % NM;
-        if (!__builtin_amdgcn_ballot_w64(g == ge && (dirty >> te & 1u))) continue;
-        typename M::Values one = val;              // the token's row, in place of the first
-#pragma unroll
-        for (int e = 1; e < NM; ++e) {
-          M::take(one, val, e, e == te);
-          one.keep(e, false);
-        }
-        one.keep(0, g == ge);
-        typename M::Turned turned;
-        M::turn(one, turned);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          if (c >= groups) continue;               // (uniform)
-          float w[NM];
-#pragma unroll
-          for (int e = 0; e < NM; ++e) w[e] = 0.f;
-#pragma unroll
-          for (int e = 0; e < NM; ++e) w[0] = e == te ? z[c][e] : w[0];
-          const bool on = __shfl(on_bits[c], n + 16 * ge, 64) >> te & 1u;
-          const auto terms = M::split(w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const v4f sum = M::add(turned, j, terms, acc[c][j]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) acc[c][j][x] = on ? sum[x] : acc[c][j][x];
-          }
-        }
-        // (its row is zeros from here on)
-#pragma unroll
-        for (int e = 0; e < NM; ++e) val.keep(e, !(g == ge && e == te));
-      }
-    }
-    typename M::Turned turned;
-    M::turn(val, turned);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (c >= groups) continue;                   // (uniform)
       const auto terms = M::split(z[c]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[c][j] = M::add(turned, j, terms, acc[c][j]);
     }
-    if (more) load_values(t1, vp1);
-    t0 = t1, vp = vp1;
-    t1 = t2, kp1 = kp2, vp1 = vp2;
   }
 
-  // The waves' sums meet in LDS, group by group.
-  const int64_t out_row = (int64_t)seq * a.drafts * p.n_q_heads + kvh * G;
-  auto finish = [&](int col, int c4, float top, float total, v4f o) {
-    const int x = cb * a.block_cols + col, i = x / G, j = x - i * G;
-    const int64_t head = out_row + (int64_t)i * p.n_q_heads + j;
-    const bool lost = top == kLowest && total == total;     // attended scores were all -infinity
-    if (lost) o = (v4f){NAN, NAN, NAN, NAN};
-    const v4f zero = {0.f, 0.f, 0.f, 0.f};
-    reinterpret_cast<v4f*>(p.out)[head * (kD / 4) + c4] = total == 0.f ? zero : o / total;
-    if (p.lse && c4 == 0)
-      p.lse[head] = total == 0.f || lost ? -INFINITY : (top + log2f(total)) * kLn2;
-  };
-  const int shared = shared_before + kvh;          // the row's first slot; part q's is heads q further
-  auto part_at = [&](int q, int col) {
-    return (((shared + q * heads) * a.blocks + cb) * a.block_cols + col) * (int)sizeof(Partial);
-  };
+  // Values that are not finite count for the columns that attend them and for no others (0 times them
+  // is NaN): the tokens of a tile that have such, one by one, with a choice behind the product.
+  __device__ void odd_values(int t0, const TreePages& pages) {
+    const int vp = pages.page_of(t0 + 8 * M::value_block(g));
+    const bool there = pages.exists(vp);
+    if (is_whole(t0, there)) return;               // (uniform)
+    typename M::Values val;
+    val.load(p.v + pages.slot_of(t0 + NM * g, vp), p.tok_stride, n);
+    const unsigned dirty = mask_values(t0, there, val);
+    if (!__builtin_amdgcn_ballot_w64(dirty != 0u)) return;
+    typename M::Keys key;
+    key.load(p.k + pages.slot_of(t0 + M::key_token(0, n), pages.page_of(t0 + 8 * M::key_block(n))),
+             p.tok_stride, g);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float z[NM];
+      M::template scores<QT>(key, q[c], z);
+      const unsigned bits = weigh(c, t0, false, there, z);
+      const float ref = m_run[c] == -INFINITY ? 0.f : m_run[c];
+      for (int tok = 0; tok < TT; ++tok) {
+        const int ge = tok / NM, te = tok % NM;
+        if (!__builtin_amdgcn_ballot_w64(g == ge && (dirty >> te & 1u))) continue;
+        typename M::Values one = val;              // the token's row, in place of the first
+        float w[NM];
+        w[0] = z[0];
+#pragma unroll
+        for (int e = 1; e < NM; ++e) {
+          M::take(one, val, e, e == te);
+          one.keep(e, false);
+          w[0] = e == te ? z[e] : w[0];
+          w[e] = 0.f;
+        }
+        one.keep(0, g == ge);
+        w[0] = __builtin_amdgcn_exp2f(w[0] - ref);
+        typename M::Turned turned;
+        M::turn(one, turned);
+        const bool on = __shfl(bits, n + 16 * ge, 64) >> te & 1u;
+        const auto terms = M::split(w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const v4f sum = M::add(turned, j, terms, acc[c][j]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) acc[c][j][x] = on ? sum[x] : acc[c][j][x];
+        }
+      }
+    }
+  }
+};
+
+// LDS of the joins: the waves' sums of a group each, rows padded for the banks; the (column, part)
+// maxima and sums of a row.
+constexpr int kSumsFloats = kGroup * (kD + 4);
+
+template <int W>
+struct TreeSpace {
+  TreeInfo info;
+  float m[W][kGroup], l[W][kGroup];
+  int scan[2][W], found[4];
+};
+
+// Four channels of a column's result.
+__device__ inline void finish_column(const TreeArgs& a, const TreeRun& r, int i, int column, int c4,
+                                     float top, float total, v4f o) {
+  const PagedArgs& p = a.p;
+  const int64_t head = ((int64_t)r.seq * a.drafts + i) * p.n_q_heads + r.kvh * p.G + column - i * p.G;
+  const bool lost = top == kLowest && total == total;       // attended scores were all -infinity
+  if (lost) o = (v4f){NAN, NAN, NAN, NAN};
+  const v4f zero = {0.f, 0.f, 0.f, 0.f};
+  reinterpret_cast<v4f*>(p.out)[head * (kD / 4) + c4] = total == 0.f ? zero : o / total;
+  if (p.lse && c4 == 0)
+    p.lse[head] = total == 0.f || lost ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+// Where part q of the row is, bytes from the workspace's first slot.
+__device__ inline int part_at(const TreeArgs& a, const TreeRun& r, int cb, int q, int col) {
+  return (((r.shared + q * a.p.n_kv_heads) * a.blocks + cb) * a.block_cols + col) * (int)sizeof(Partial);
+}
+
+// What becomes of the waves' sums: waves w TW .. w TW + TW - 1 have the same columns (C groups from
+// w 16 C on) and different tokens.  sums(wave): kSumsFloats of LDS.
+template <int W, int TW, class Wave, class Sums, int C>
+__device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, int cb, int columns,
+                                           TreeSpace<W>& sh, Wave& x, Sums sums,
+                                           std::integral_constant<int, C>) {
+  constexpr int NT = 64 * W, CW = W / TW;
+  using M = typename Wave::Tile;
+  const PagedArgs& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if (c >= groups) continue;                     // (uniform)
-    __syncthreads();                               // the queries, or the last group's sums, are read
-    float l = over_groups_sum(l_run[c]);
-    float top = m_run[c];
-    unsigned any = seen >> c & 1u;
+    __syncthreads();                               // the tiles, or the last group's sums, are read
+    const float l = over_groups_sum(x.l_run[c]);
+    unsigned any = x.seen >> c & 1u;
     any |= __shfl_xor(any, 16, 64);
     any |= __shfl_xor(any, 32, 64);
-    if (any && top == -INFINITY && l == 0.f) {     // (NaN scores: the sum is NaN)
-      top = kLowest;
-      l = 1.f;
-    }
+    // (NaN scores: the sum is NaN)
+    const bool low = any && x.m_run[c] == -INFINITY && l == 0.f;
     if (g == 0) {
-      sh.m[wave][n] = top;
-      sh.l[wave][n] = l;
+      sh.m[wave][n] = low ? kLowest : x.m_run[c];
+      sh.l[wave][n] = low ? 1.f : l;
     }
+    float* mine = sums(wave) + n * (kD + 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sh.sums[wave][n][M::channel(j, i, g)] = acc[c][j][i];
+      for (int i = 0; i < 4; ++i) mine[M::channel(j, i, g)] = x.acc[c][j][i];
     __syncthreads();
-    const int h = tid / (kD / 4), c4 = tid % (kD / 4), col = c * kGroup + h;
-    static_assert(NT == kGroup * (kD / 4), "a thread for every four channels of a group");
-    float mm = sh.m[0][h];
+    for (int y = tid; y < CW * kGroup * (kD / 4); y += NT) {
+      const int h = y / (kD / 4) % kGroup, c4 = y % (kD / 4), w0 = y / (kGroup * (kD / 4)) * TW;
+      const int col = (w0 / TW * C + c) * kGroup + h;
+      float mm = sh.m[w0][h];
 #pragma unroll
-    for (int w = 1; w < W; ++w) mm = fmaxf(mm, sh.m[w][h]);
-    float ll = 0.f;
-    v4f o = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 1; w < TW; ++w) mm = fmaxf(mm, sh.m[w0 + w][h]);
+      float ll = 0.f;
+      v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const float f = sh.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[w][h] - mm);
-      ll += sh.l[w][h] == 0.f ? 0.f : f * sh.l[w][h];
-      o += f * *reinterpret_cast<const v4f*>(&sh.sums[w][h][4 * c4]);
-    }
-    if (col < columns) {
-      if (parts == 1) {
-        finish(col, c4, mm, ll, o);
+      for (int w = 0; w < TW; ++w) {
+        const float m = sh.m[w0 + w][h], lw = sh.l[w0 + w][h];
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+        ll += lw == 0.f ? 0.f : f * lw;
+        o += f * *reinterpret_cast<const v4f*>(sums(w0 + w) + h * (kD + 4) + 4 * c4);
+      }
+      if (col >= columns) continue;
+      if (r.parts == 1) {
+        finish_column(a, r, sh.info.draft[col], cb * a.block_cols + col, c4, mm, ll, o);
       } else {
-        const int off = part_at(part, col);
-        __builtin_amdgcn_raw_buffer_store_b128((v4i)o, slots, off + 16 + 16 * c4, 0, kCoherent);
-        if (c4 == 0)
-          __builtin_amdgcn_raw_buffer_store_b128((v4i)(v4f){mm, ll, 0.f, 0.f}, slots, off, 0,
-                                                 kCoherent);
+        v4f* slot = reinterpret_cast<v4f*>(reinterpret_cast<char*>(a.p.parts) +
+                                           part_at(a, r, cb, r.part, col));
+        slot[1 + c4] = o;
+        if (c4 == 0) slot[0] = (v4f){mm, ll, 0.f, 0.f};
       }
     }
   }
-  if (parts == 1) return;
+}
 
-  // The last of the row's workgroups joins them, in the order of the parts.
-  unsigned* counter = p.counters + ((int64_t)shared * a.blocks + cb) * kTreeCounterStride;
-  __builtin_amdgcn_s_waitcnt(0);                   // this thread's stores are done
-  __syncthreads();
-  if (tid == 0)
-    sh.arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (sh.arrived != (unsigned)parts - 1u) return;  // (uniform)
+// The parts of the rows that are shared, joined in their order: the same grid as the runs', and as many
+// workgroups as a row has parts take a share of its columns each.  (A join by the last of a row's
+// workgroups would read up to 4 MiB alone: 100 us at 32 parts of 256 columns.)
+constexpr int kJoinWaves = 8;
+
+template <int TT>
+__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) {
+  constexpr int W = kJoinWaves, NT = 64 * W;
+  constexpr int kPairs = kMostCols + kTreeGroups;  // columns / parts of them, for each part
+  __shared__ int scan[2][W], found[4];
+  __shared__ float weight[kPairs], sum[kPairs], top[kMostCols], total[kMostCols];
+  const PagedArgs& p = a.p;
+  const int tid = threadIdx.x, block = (int)blockIdx.x;
+  const int unit = (block >> 3) / a.blocks * 8 + (block & 7), cb = (block >> 3) % a.blocks;
+  TreeRun r;
+  if (!find_run<TT, W>(a, unit, scan, found, r) || r.parts == 1) return;
+  const int columns = min(r.m * p.G - cb * a.block_cols, a.block_cols), parts = r.parts;
+  if (columns <= 0) return;
+  const int first = columns * r.part / parts, count = columns * (r.part + 1) / parts - first;
+  const char* slots = reinterpret_cast<const char*>(p.parts);
   auto slot = [&](int q, int col, int off) {
-    return (v4f)__builtin_amdgcn_raw_buffer_load_b128(slots, part_at(q, col) + off, 0, kCoherent);
+    return *reinterpret_cast<const v4f*>(slots + part_at(a, r, cb, q, first + col) + off);
   };
-  for (int x = tid; x < columns * parts; x += NT) {
-    const v4f ml = slot(x / columns, x % columns, 0);
-    sh.parts.m[x] = ml[0];
-    sh.parts.l[x] = ml[1];
+  constexpr int U = 8;                             // parts in flight, the first before their weights
+  v4f v[U];
+  auto fetch = [&](int y, int q0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = slot(min(q0 + u, parts - 1), min(y / (kD / 4), count - 1), 16 + 16 * (y % (kD / 4)));
+  };
+  if (count > 0) fetch(tid, 0);
+  for (int y = tid; y < count * parts; y += NT) {
+    const v4f ml = slot(y % parts, y / parts, 0);
+    weight[y] = ml[0];
+    sum[y] = ml[1];
   }
   __syncthreads();
-  for (int col = tid >> 3; col < columns; col += NT / 8) {        // eight threads a column
-    float top = -INFINITY, total = 0.f;
+  for (int col = tid >> 3; col < count; col += NT / 8) {           // eight threads a column
+    float m = -INFINITY, l = 0.f;
     for (int q = tid & 7; q < parts; q += 8)
-      if (sh.parts.l[q * columns + col] != 0.f) top = fmaxf(top, sh.parts.m[q * columns + col]);
+      if (sum[col * parts + q] != 0.f) m = fmaxf(m, weight[col * parts + q]);
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float ref = top == -INFINITY ? 0.f : top;
+    for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float ref = m == -INFINITY ? 0.f : m;
     for (int q = tid & 7; q < parts; q += 8) {
-      const float l = sh.parts.l[q * columns + col];
-      const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sh.parts.m[q * columns + col] - ref);
-      total += l == 0.f ? 0.f : w * l;             // (NaN stays)
-      sh.parts.m[q * columns + col] = w;
+      const float s = sum[col * parts + q];
+      const float w = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(weight[col * parts + q] - ref);
+      l += s == 0.f ? 0.f : w * s;                 // (NaN stays)
+      weight[col * parts + q] = w;
     }
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) total += __shfl_xor(total, o, 64);
+    for (int o = 1; o < 8; o <<= 1) l += __shfl_xor(l, o, 64);
     if ((tid & 7) == 0) {
-      sh.top[col] = top;
-      sh.total[col] = total;
+      top[col] = m;
+      total[col] = l;
     }
   }
   __syncthreads();
-  constexpr int U = 8;                             // parts in flight
-  for (int x = tid; x < columns * (kD / 4); x += NT) {
-    const int col = x / (kD / 4), c4 = x % (kD / 4);
+  for (int y = tid; y < count * (kD / 4); y += NT) {
+    const int col = y / (kD / 4), c4 = y % (kD / 4);
     v4f o = {0.f, 0.f, 0.f, 0.f};
     for (int q0 = 0; q0 < parts; q0 += U) {
-      v4f v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = slot(min(q0 + u, parts - 1), col, 16 + 16 * c4);
+      if (q0 > 0 || y != tid) fetch(y, q0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float w = q0 + u < parts ? sh.parts.m[(q0 + u) * columns + col] : 0.f;
+        const float w = q0 + u < parts ? weight[col * parts + q0 + u] : 0.f;
         if (w != 0.f) o += w * v[u];
       }
     }
-    finish(col, c4, sh.top[col], sh.total[col], o);
+    const int column = cb * a.block_cols + first + col;
+    finish_column(a, r, column / p.G, column, c4, top[col], total[col], o);
   }
-  if (tid == 0) *counter = 0u;                     // as the next call expects it
 }
 
-// A (sequence, KV head)'s columns in blocks of nearly as many groups each.
+// Up to 16 columns: eight waves, each with tiles of its own; keys and values one tile ahead, pages
+// two.
+template <class M, int QT>
+__global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
+  constexpr int W = 8, TT = M::kTokens, NM = M::kMine;
+  __shared__ TreeSpace<W> sh;
+  __shared__ __align__(16) float space[W * kSumsFloats];
+  const PagedArgs& p = a.p;
+  const int n = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  TreeRun r;
+  if (!find_run<TT, W>(a, (int)blockIdx.x, sh.scan, sh.found, r)) return;
+  const int columns = r.m * p.G;
+  const TreePages pages(p, r.seq, r.kvh);
+  typename M::Keys key;
+  typename M::Values val;
+  auto load_keys = [&](int t0, int page) {
+    key.load(p.k + pages.slot_of(t0 + M::key_token(0, n), page), p.tok_stride, g);
+  };
+  auto load_values = [&](int t0, int page) {
+    val.load(p.v + pages.slot_of(t0 + NM * g, page), p.tok_stride, n);
+  };
+  auto key_page = [&](int t0) { return pages.page_of(t0 + 8 * M::key_block(n)); };
+  auto value_page = [&](int t0) { return pages.page_of(t0 + 8 * M::value_block(g)); };
+  const int begin = r.first + wave, last = r.last;
+  int t0 = r.rt.token(min(begin, last - 1), TT), t1 = r.rt.token(min(begin + W, last - 1), TT);
+  int vp = value_page(t0), kp1 = key_page(t1), vp1 = value_page(t1);
+  if (begin < last) {
+    load_keys(t0, key_page(t0));
+    load_values(t0, vp);
+  }
+  TreeWave<M, QT, 1> x(a, r, sh.info, 0, 0, columns);
+  if (wave == W - 1) find_families(a, r, sh.info);
+  __syncthreads();
+  for (int i = begin; i < last; i += W) {
+    const bool more = i + W < last;
+    const int t2 = r.rt.token(min(i + 2 * W, last - 1), TT);
+    int kp2, vp2;
+    x.step(t0, pages.exists(vp), key, val,
+           [&] { if (more) load_values(t1, vp1); },
+           [&] {
+             if (more) load_keys(t1, kp1);
+             kp2 = key_page(t2), vp2 = value_page(t2);
+           });
+    t0 = t1, vp = vp1;
+    t1 = t2, kp1 = kp2, vp1 = vp2;
+  }
+  if (x.odd)
+    for (int i = begin; i < last; i += W) x.odd_values(r.rt.token(i, TT), pages);
+  finish_run<W, W>(a, r, 0, columns, sh, x, [&](int w) { return space + w * kSumsFloats; },
+                   std::integral_constant<int, 1>{});
+}
+
+// More columns.  A stage has kStage tiles: 16 KiB of keys and 16 KiB of values, loaded straight into
+// LDS, kRing - 1 stages ahead of the one that is computed.  Wave w has 16 C columns from
+// (w / TW) 16 C on and every TW-th tile.
+constexpr int kStage = 2, kRing = 4;
+constexpr int kHalfStage = kStage * 8192;          // bytes of a stage's keys, and of its values
+// Waits until no more than n vector loads are outstanding, and for LDS.
+template <int N>
+__device__ inline void wait_loads() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4 << 14));
+}
+
+// The keys and values of a tile in LDS.  (In assembly, with the wait: the compiler would wait for the
+// loads of the next stage too, which go elsewhere in the same array.)
+template <class M>
+__device__ inline void read_keys(typename M::Keys& to, uint32_t even, uint32_t odd) {
+  v4u x[8];
+  static_assert(sizeof to == sizeof x, "eight pieces");
+  asm volatile(
+      "ds_read_b128 %0, %8 offset:%10\n\tds_read_b128 %1, %9 offset:%11\n\t"
+      "ds_read_b128 %2, %8 offset:%12\n\tds_read_b128 %3, %9 offset:%13\n\t"
+      "ds_read_b128 %4, %8 offset:%14\n\tds_read_b128 %5, %9 offset:%15\n\t"
+      "ds_read_b128 %6, %8 offset:%16\n\tds_read_b128 %7, %9 offset:%17\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+        "=&v"(x[7])
+      : "v"(even), "v"(odd), "n"(M::key_offset(0)), "n"(M::key_offset(1)), "n"(M::key_offset(2)),
+        "n"(M::key_offset(3)), "n"(M::key_offset(4)), "n"(M::key_offset(5)), "n"(M::key_offset(6)),
+        "n"(M::key_offset(7))
+      : "memory");
+  __builtin_memcpy(&to, x, sizeof x);
+}
+template <class M>
+__device__ inline void read_values(typename M::Values& to, const uint32_t (&at)[4]) {
+  v4u x[8];
+  static_assert(sizeof to == sizeof x, "eight pieces");
+  asm volatile(
+      "ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%17\n\t"
+      "ds_read_b128 %2, %10 offset:%18\n\tds_read_b128 %3, %11 offset:%19\n\t"
+      "ds_read_b128 %4, %12 offset:%20\n\tds_read_b128 %5, %13 offset:%21\n\t"
+      "ds_read_b128 %6, %14 offset:%22\n\tds_read_b128 %7, %15 offset:%23\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+        "=&v"(x[7])
+      : "v"(at[M::value_turn(0)]), "v"(at[M::value_turn(1)]), "v"(at[M::value_turn(2)]),
+        "v"(at[M::value_turn(3)]), "v"(at[M::value_turn(4)]), "v"(at[M::value_turn(5)]),
+        "v"(at[M::value_turn(6)]), "v"(at[M::value_turn(7)]), "n"(kHalfStage + M::value_offset(0)),
+        "n"(kHalfStage + M::value_offset(1)), "n"(kHalfStage + M::value_offset(2)),
+        "n"(kHalfStage + M::value_offset(3)), "n"(kHalfStage + M::value_offset(4)),
+        "n"(kHalfStage + M::value_offset(5)), "n"(kHalfStage + M::value_offset(6)),
+        "n"(kHalfStage + M::value_offset(7))
+      : "memory");
+  __builtin_memcpy(&to, x, sizeof x);
+}
+
+template <class M, int QT, int C, int CW, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
+  constexpr int TT = M::kTokens, NM = M::kMine, TW = W / CW;
+  constexpr int kRow = M::kRow;
+  constexpr int PT = kStage * TT / W;              // tokens of a stage that a wave loads
+  constexpr int kPer = 1024 / kRow;                // tokens of one load of the wave
+  static_assert(TW >= 1 && TW <= kStage && 16 * C * CW <= kMostCols, "a tile for every wave");
+  __shared__ TreeSpace<W> sh;
+  __shared__ __align__(1024) char ring[kRing * 2 * kHalfStage];
+  __shared__ int there[kRing][kStage * TT / 8];    // whether the page of 8 tokens is
+  const PagedArgs& p = a.p;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The column blocks of one run read the same tokens: they are on one XCD (workgroups go to the
+  // eight in turn) at one time, and meet in its L2.
+  const int block = (int)blockIdx.x;
+  const int unit = (block >> 3) / a.blocks * 8 + (block & 7), cb = (block >> 3) % a.blocks;
+  TreeRun r;
+  if (!find_run<TT, W>(a, unit, sh.scan, sh.found, r)) return;
+  const int columns = min(r.m * p.G - cb * a.block_cols, a.block_cols);
+  if (columns <= 0) return;                        // (uniform)
+  const TreePages pages(p, r.seq, r.kvh);
+
+  // This wave's PT tokens of a stage: their first one, pages a stage ahead of the loads, and those.
+  // (Pages by scalar loads: a vector load's wait would be one for all loads before it.  Every stage has
+  // as many loads, so that they can be counted; behind the last tile it is that one again.)
+  const int tile = wave * PT / TT, within = wave * PT % TT;
+  const auto row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)pages.row;
+  int page[PT / 8];
+  auto token_of = [&](int s) {
+    return r.rt.token(min(r.first + s * kStage + tile, r.last - 1), TT) + within;
+  };
+  auto fetch_pages = [&](int s) {
+    const int t = token_of(s);
+#pragma unroll
+    for (int b = 0; b < PT / 8; ++b) {
+      const int i = __builtin_amdgcn_readfirstlane((t + 8 * b) >> p.page_shift);
+      page[b] = i < p.max_pages ? row[i] : -1;
+    }
+  };
+  constexpr int kLoads = 2 * PT / kPer;            // of a stage, of a wave
+  auto issue = [&](int s) {
+    const int t = token_of(s), slot = s % kRing;
+#pragma unroll
+    for (int i = 0; i < PT / kPer; ++i) {
+      const int at = i * kPer + lane / (kRow / 16), c = lane % (kRow / 16);
+      const int64_t from = pages.slot_of(t + at, page[i * kPer / 8]) +
+                           16 * (c ^ M::turn_of((wave * PT + at) % TT));
+      char* to = ring + slot * (2 * kHalfStage) + (wave * PT + i * kPer) * kRow;
+      using Global = const __attribute__((address_space(1))) void*;
+      using Local = __attribute__((address_space(3))) void*;
+      __builtin_amdgcn_global_load_lds((Global)(p.k + from), (Local)to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kHalfStage), 16, 0, 0);
+    }
+    if (lane < PT / 8) {
+      int on = 0;
+#pragma unroll
+      for (int b = 0; b < PT / 8; ++b) on = lane == b ? pages.exists(page[b]) : on;
+      there[slot][wave * PT / 8 + lane] = on;
+    }
+  };
+
+  const int stages = (r.last - r.first + kStage - 1) / kStage;
+#pragma unroll 1
+  for (int s = 0; s < kRing - 1; ++s) {
+    fetch_pages(s);
+    issue(s);
+  }
+  fetch_pages(kRing - 1);
+  const int cw = wave / TW, tw = wave % TW;
+  TreeWave<M, QT, C> x(a, r, sh.info, cb, cw * C * kGroup, columns);
+  if (wave == W - 1) find_families(a, r, sh.info);
+  const bool busy = cw * C * kGroup < columns;     // (uniform)
+  // Where the lane's pieces of a tile are (the ring is aligned to more than a row: the turns of the
+  // value pieces flip bits 4 and 5 of the address).
+  const uint32_t key0 = M::key_place(0, n, g), key1 = M::key_place(1, n, g);
+  const uint32_t value0 = M::value_place(0, n, g);
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+#pragma unroll 1
+  for (int s = 0; s < stages; ++s) {
+    wait_loads<(kRing - 2) * kLoads>();            // this wave's part of the stage has come
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();                  // everyone's has, and the stage before is read
+    asm volatile("" ::: "memory");
+    issue(s + kRing - 1);
+    fetch_pages(s + kRing);
+    const int slot = s % kRing;
+    if (busy)
+#pragma unroll 1
+      for (int k = tw; k < kStage; k += TW) {
+        const int i = r.first + s * kStage + k;
+        if (i >= r.last) break;                    // (uniform)
+        typename M::Keys key;
+        typename M::Values val;
+        const uint32_t from = base + slot * (2 * kHalfStage) + k * (TT * kRow);
+        const uint32_t value_at[4] = {from + value0, (from + value0) ^ 16u, (from + value0) ^ 32u,
+                                      (from + value0) ^ 48u};
+        read_keys<M>(key, from + key0, from + key1);
+        read_values<M>(val, value_at);
+        x.step(r.rt.token(i, TT), there[slot][k * TT / 8 + M::value_block(g)] != 0, key, val, [] {}, [] {});
+      }
+  }
+  wait_loads<0>();                                 // (the loads behind the last stage)
+  if (x.odd)
+    for (int i = r.first + tw; i < r.last; i += TW) x.odd_values(r.rt.token(i, TT), pages);
+  finish_run<W, TW>(a, r, cb, columns, sh, x,
+                    [&](int w) { return reinterpret_cast<float*>(ring) + w * kSumsFloats; },
+                    std::integral_constant<int, C>{});
+}
+
+// A (sequence, KV head)'s columns in blocks of nearly as many groups each; a block's groups are dealt
+// to `cw` sets of waves, c groups each.  `most`: groups of a block.  Sixteen where two waves a SIMD have
+// room for two groups each (queries of one 16-bit term), else eight.
 struct Blocks {
-  int blocks, cols;
+  int blocks, c, cw;
+  int cols() const { return c * cw * kGroup; }
 };
-Blocks blocks_of(int drafts, int G) {
+constexpr int kMostSame = 16, kMostOther = 8;
+Blocks blocks_of(int drafts, int G, int most) {
   const int groups = (drafts * G + kGroup - 1) / kGroup;
-  const int blocks = (groups + kMostGroups - 1) / kMostGroups;
-  return {blocks, (groups + blocks - 1) / blocks * kGroup};
+  if (groups == 1) return {1, 1, 1};
+  const int blocks = (groups + most - 1) / most, each = (groups + blocks - 1) / blocks;
+  return {blocks, each <= 4 ? 1 : 2, each <= 8 ? 4 : 8};
 }
 int units_of(int blocks) { return std::max(1, kTreeGroups / blocks); }
 
-size_t tree_parts_bytes(const Blocks& b) {
-  return (size_t)kTreeSlots * b.cols * sizeof(Partial);
+size_t tree_parts_bytes(const Blocks& b, int64_t rows) {
+  const int slots = rows <= units_of(b.blocks) ? kTreeGroups : kTreeSlots;
+  return (size_t)slots * b.cols() * sizeof(Partial);
 }
 
 }  // namespace
 
-size_t tree_workspace_bytes(int, int drafts, int n_q_heads, int n_kv_heads) {
-  return kTreeCountersBytes + tree_parts_bytes(blocks_of(drafts, n_q_heads / n_kv_heads));
+size_t tree_workspace_bytes(int batch, int drafts, int n_q_heads, int n_kv_heads) {
+  const int G = n_q_heads / n_kv_heads;
+  const int64_t rows = (int64_t)batch * n_kv_heads;
+  return std::max(tree_parts_bytes(blocks_of(drafts, G, kMostSame), rows),
+                  tree_parts_bytes(blocks_of(drafts, G, kMostOther), rows));
 }
 
 bool tree_fits(int64_t batch, int drafts, int n_q_heads, int n_kv_heads) {
   const int64_t columns = (int64_t)drafts * (n_q_heads / n_kv_heads);
   if (columns > kMaxColumns) return false;
-  const Blocks b = blocks_of(drafts, n_q_heads / n_kv_heads);
+  const Blocks b = blocks_of(drafts, n_q_heads / n_kv_heads, kMostOther);
   return (batch * n_kv_heads + kTreeGroups + 8) * b.blocks <= kMaxTreeGroups;
 }
 
 aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
-  const Blocks b = blocks_of(a.drafts, a.p.G);
-  a.blocks = b.blocks;
-  a.block_cols = b.cols;
-  a.units = units_of(b.blocks);
-  a.p.counters = static_cast<unsigned*>(workspace);
-  a.p.parts = reinterpret_cast<Partial*>(static_cast<char*>(workspace) + kTreeCountersBytes);
-  a.p.parts_bytes = (int)tree_parts_bytes(b);
-  // Rows that fit the chip are cut into runs that do; more rows into runs as long as the average
-  // share: no more than `units` of them beyond one a row.
+  const bool same = a.p.q_dtype == (int)c_dtype, full = c_dtype == AATC_F32;
+  const Blocks b = blocks_of(a.drafts, a.p.G, same && !full ? kMostSame : kMostOther);
   const int rows = a.p.batch * a.p.n_kv_heads;
+  a.blocks = b.blocks;
+  a.block_cols = b.cols();
+  a.units = units_of(b.blocks);
+  a.quantum = b.cols() == kGroup ? kNarrowQuantum : kWideQuantum;
+  a.p.parts = static_cast<Partial*>(workspace);
   const int64_t most = rows <= a.units ? a.units : (int64_t)rows + a.units;
   const int64_t grid = (most + 7) / 8 * 8 * b.blocks;
-  auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kTreeWaves), 0, (hipStream_t)stream, a);
+  const hipStream_t st = (hipStream_t)stream;
+  auto launch = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * waves), 0, st, a);
     return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
   };
   auto launch_as = [&](auto m, auto qt) {
     using M = decltype(m);
     constexpr int QT = decltype(qt)::value;
-    switch (b.cols / kGroup) {
-      case 1: return launch(tree_kernel<M, QT, 1>);
-      case 2: return launch(tree_kernel<M, QT, 2>);
-      default: return launch(tree_kernel<M, QT, 4>);
+    // Queries of one 16-bit term leave room for two waves a SIMD.
+    constexpr int W = QT == 1 && sizeof(typename M::Elem) == 2 ? 8 : 4;
+    switch (10 * b.cw + b.c) {
+      case 11: return launch(tree_narrow_kernel<M, QT>, 8);
+      case 41: return launch(tree_wide_kernel<M, QT, 1, 4, W>, W);
+      case 42: return launch(tree_wide_kernel<M, QT, 2, 4, W>, W);
+      default:
+        if constexpr (W == 8) return launch(tree_wide_kernel<M, QT, 2, 8, W>, W);
+        else return AATC_E_UNSUPPORTED;            // (no such block)
     }
   };
   using One = std::integral_constant<int, 1>;
   using Three = std::integral_constant<int, 3>;
-  const bool same = a.p.q_dtype == (int)c_dtype;
-  auto launch_type = [&](auto far) {
-    constexpr bool F = decltype(far)::value;
-    switch (c_dtype) {
-      case AATC_F32: return launch_as(Full32<F>{}, One{});
-      case AATC_BF16:
-        return same ? launch_as(Half16<__bf16, F>{}, One{}) : launch_as(Half16<__bf16, F>{}, Three{});
-      default:
-        return same ? launch_as(Half16<_Float16, F>{}, One{})
-                    : launch_as(Half16<_Float16, F>{}, Three{});
-    }
-  };
-  return launch_type(std::false_type{});
+  const aatc_status e =
+      full ? launch_as(Full32<false>{}, One{})
+      : c_dtype == AATC_BF16 ? same ? launch_as(Half16<__bf16, false>{}, One{})
+                                    : launch_as(Half16<__bf16, false>{}, Three{})
+      : same ? launch_as(Half16<_Float16, false>{}, One{})
+             : launch_as(Half16<_Float16, false>{}, Three{});
+  // (a table that holds no more than a shortest run's tokens has no shared rows)
+  const int tt = full ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
+  if (e != AATC_OK || (a.p.len_max + a.drafts) / tt < kRoundsMin * a.quantum) return e;
+  return full ? launch(tree_join_kernel<Full32<false>::kTokens>, kJoinWaves)
+              : launch(tree_join_kernel<Half16<__bf16, false>::kTokens>, kJoinWaves);
 }
 
 namespace {

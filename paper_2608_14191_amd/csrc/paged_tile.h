@@ -86,6 +86,22 @@ struct Half16 {
   static __device__ int key_token(int u, int n) { return 8 * (n >> 2) + 4 * u + (n & 3); }
   static __device__ int key_block(int n) { return n >> 2; }
   static __device__ int value_block(int g) { return g; }
+  // A tile in LDS: piece c (16 bytes) of a token's row lies in the place c ^ turn_of(row), so that
+  // the eight rows that a quarter of a wave reads a key operand from are in different banks.  Register
+  // u (of eight) of a lane's keys is at key_place(u & 1) + key_offset(u), of its values at
+  // value_place(value_turn(u)) + value_offset(u).
+  static constexpr int kRow = 256;
+  static __device__ int turn_of(int row) { return (row & 3) | (row >> 1 & 4); }
+  static __device__ int key_place(int odd, int n, int g) {
+    const int row = key_token(0, n), t = turn_of(row);
+    return row * kRow + 16 * (g ^ (t & 3)) + 64 * (odd ^ (t >> 2));
+  }
+  static constexpr int key_offset(int u) { return u / 4 * 4 * kRow + u % 4 / 2 * 128; }
+  static __device__ int value_place(int turn, int n, int g) {
+    return 8 * g * kRow + 16 * (n ^ (turn_of(8 * g) | turn));
+  }
+  static constexpr int value_turn(int u) { return u & 3; }
+  static constexpr int value_offset(int u) { return u * kRow; }
 
   static __device__ v4f mfma(v8 a, v8 b, v4f c) {
     if constexpr (kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -205,7 +221,10 @@ struct Half16 {
       if constexpr (kF16) {
         const auto top = __builtin_amdgcn_cvt_pkrtz(x, y);
         typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-        const v2h rest = {(_Float16)(x - (float)top[0]), (_Float16)(y - (float)top[1])};
+        float a, b;                                // x - top[0], y - top[1] (exact)
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(a) : "v"(top), "v"(x));
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(b) : "v"(top), "v"(y));
+        const v2h rest = {(_Float16)a, (_Float16)b};
         w.t[0][d] = __builtin_bit_cast(uint32_t, top);
         w.t[1][d] = __builtin_bit_cast(uint32_t, rest);
       } else {
@@ -229,6 +248,18 @@ struct Half16 {
   static __device__ void take(Values& to, const Values& v, int e, bool on) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) to.r[0][i] = on ? v.r[e][i] : to.r[0][i];
+  }
+  // Whether any of the lane's values may be not finite (all bits of the exponent in some element).
+  static __device__ bool any_bad(const Values& v) {
+    typedef uint16_t v2 __attribute__((ext_vector_type(2)));
+    const uint32_t up = kF16 ? 0x7c007c00u : 0x7f807f80u;
+    v2 most = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(v2, v.r[e][d] & up));
+    return most[0] == (up & 0xffffu) || most[1] == (up & 0xffffu);
   }
   // Whether the lane's part of token e is not finite.
   static __device__ bool bad(const Values& v, int e) {
@@ -273,6 +304,19 @@ struct Full32 {
   static __device__ int key_token(int, int n) { return n; }
   static __device__ int key_block(int n) { return n >> 3; }
   static __device__ int value_block(int g) { return g >> 1; }
+  // (as Half16's)
+  static constexpr int kRow = 512;
+  static __device__ int turn_of(int row) { return row & 7; }
+  static __device__ int key_place(int odd, int n, int g) {
+    const int t = turn_of(n);
+    return n * kRow + 16 * (g ^ (t & 3)) + 64 * (odd ^ (t >> 2));
+  }
+  static constexpr int key_offset(int u) { return u / 2 * 128; }
+  static __device__ int value_place(int turn, int n, int g) {
+    return 4 * g * kRow + 16 * (n ^ (turn_of(4 * g) | turn));
+  }
+  static constexpr int value_turn(int u) { return u / 2; }
+  static constexpr int value_offset(int u) { return u / 2 * kRow + u % 2 * 256; }
   static __device__ v4f mfma(float a, float b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
   }
@@ -346,6 +390,16 @@ struct Full32 {
     for (int c = 0; c < 2; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) to.r[0][c][i] = on ? v.r[e][c][i] : to.r[0][c][i];
+  }
+  static __device__ bool any_bad(const Values& v) {
+    float most = 0.f;                              // (x - x is not 0 for those alone)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most += v.r[e][c][i] - v.r[e][c][i];
+    return !(most == 0.f);
   }
   static __device__ bool bad(const Values& v, int e) {
     bool b = false;
