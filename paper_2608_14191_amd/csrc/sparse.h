@@ -32,7 +32,8 @@ struct SparseArgs {
   PagedArgs p;
   const int8_t* codes;
   const float* scales;
-  uint32_t* keys;                 // [batch][n_kv_heads][max_pages] in the order of the scores
+  uint32_t* keys;                 // [batch][n_kv_heads][key_stride], in the order of the scores
+  int64_t key_stride;
   int32_t* picked;                // [batch][n_kv_heads][most]
   int most, first, last;
   int run;                        // tiles of a workgroup at most

@@ -22,6 +22,22 @@ namespace {
 
 constexpr int kLowestStep = -50, kHighestStep = 100;
 
+// Over a wave, by shifts within rows of 16 lanes and broadcasts of rows' last lanes: lane l gets f of the
+// lanes up to l (the last one f of all).  `none`: what f leaves as it is.
+template <class F>
+__device__ inline int wave_scan(int x, int none, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));      // row_shr:1
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));      // row_bcast:15
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));      // row_bcast:31
+  return x;
+}
+__device__ inline int wave_scan_sum(int x) {
+  return wave_scan(x, 0, [](int a, int b) { return a + b; });
+}
+
 // The exponent of the smallest power of two, from 2^-50 on, of which 127 reach `top` (finite, >= 0).
 __device__ inline int step_of(float top) {
   const uint32_t bits = __float_as_uint(top);
@@ -191,14 +207,12 @@ __device__ inline Say say_of(const PagedArgs& p, int64_t at, bool on, int g) {
   return s;
 }
 
-// A workgroup of four waves scores kChunk pages of a (sequence, KV head), a wave 16 of them at a
-// time.  Reads 260 bytes a page: the memory bounds it, or the launch.  ONE: at most 16 query heads a
-// KV head, in registers; else in LDS.
-constexpr int kChunk = 256;
-
-template <bool ONE>
+// A workgroup of four waves scores 64 R pages of a (sequence, KV head), a wave 16 of them at a time.
+// Reads 260 bytes a page: the memory bounds it, or the latency of three loads in series (the length with
+// entries and queries, bounds).  ONE: at most 16 query heads a KV head, in registers; else in LDS.
+template <bool ONE, int R>
 __global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
-  constexpr int HG = ONE ? 1 : kMaxSay / 16;
+  constexpr int HG = ONE ? 1 : kMaxSay / 16, kChunk = 64 * R;
   __shared__ v4i ops[ONE ? 1 : HG][4][64];
   __shared__ int exps[HG][16];
   const PagedArgs& p = a.p;
@@ -207,20 +221,19 @@ __global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
   const int chunks = (p.max_pages + kChunk - 1) / kChunk;
   const int row = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x % chunks;
   const int seq = row / p.n_kv_heads, kvh = row % p.n_kv_heads;
-  const int len = min(max(p.seq_len[seq], 0), p.len_max);
-  const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
-  if (pages <= a.most || chunk * kChunk >= pages) return;      // (all are picked; none here)
 
-  // The wave's four tiles of pages: entries, then bounds.
-  constexpr int R = kChunk / 64;
+  // The wave's tiles of pages: entries (of all there are, before the length is known), then bounds.
   const int base = chunk * kChunk + wave * 16 * R;
   int page[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int i = base + 16 * r + n;
-    page[r] = i < pages ? p.table[seq * p.table_stride + i] : -1;
-    if (page[r] >= p.n_pages) page[r] = -1;
-  }
+  for (int r = 0; r < R; ++r)
+    page[r] = p.table[seq * p.table_stride + min(base + 16 * r + n, p.max_pages - 1)];
+  const int len = min(max(p.seq_len[seq], 0), p.len_max);
+  const int pages = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+  if (pages <= a.most || chunk * kChunk >= pages) return;      // (all are picked; none here)
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    page[r] = base + 16 * r + n < pages && page[r] < p.n_pages ? page[r] : -1;
   v4i x[R][4];
   float scale[R];
 #pragma unroll
@@ -280,7 +293,7 @@ __global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
     if (n < 4 && i < pages) {
       const float score = steps == INFINITY ? INFINITY : mine == -INFINITY ? 0.f : mine * steps;
       const bool always = i < a.first || i >= pages - a.last;
-      a.keys[(int64_t)row * p.max_pages + i] = !there ? 0u : always ? kAlways : key_of(score);
+      a.keys[row * a.key_stride + i] = !there ? 0u : always ? kAlways : key_of(score);
     }
   }
 }
@@ -290,6 +303,7 @@ __global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
 constexpr int kSparseWaves = 8, kSparseGroups = 256, kSparseCounterStride = 64;
 constexpr size_t kSparseCountersBytes = (size_t)kSparseGroups * kSparseCounterStride * sizeof(unsigned);
 constexpr int kHeldKeys = 16;                      // keys of a thread in registers
+constexpr int kBins = 1024;                        // of a pass of the choice: 10 bits of the keys
 constexpr int kListed = 2048;                      // picked pages of a workgroup in LDS
 
 // A row (a sequence, a KV head, up to 16 of its query heads) has `parts` workgroups.  Each of them finds
@@ -300,7 +314,7 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
   constexpr int W = kSparseWaves, NT = 64 * W, TT = M::kTokens, NM = M::kMine;
   __shared__ JoinSpace<W, kSparseGroups> sh;
   __shared__ int list_entry[kListed], list_page[kListed];
-  __shared__ int counts[2][W], packed[kHeldKeys * W];
+  __shared__ int hist[2][kBins], sums[3][W], found[3];
   __shared__ unsigned arrived;
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -312,7 +326,7 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
   const int shift = p.page_shift;
   const int pages = (len + (1 << shift) - 1) >> shift;
   const int32_t* table = p.table + seq * p.table_stride;
-  const uint32_t* keys = a.keys + (int64_t)pair * p.max_pages;
+  const uint32_t* keys = a.keys + pair * a.key_stride;
   auto exists = [&](int page) { return (page >= 0) & (page < p.n_pages); };
 
   // Queries early: their loads take as long as the choice.
@@ -322,55 +336,127 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
          seq * p.q_stride + ((int64_t)kvh * p.G + hgi * kPagedHeads + min(n, heads - 1)) * kD,
          n < heads, g);
 
+  // Thread t has the keys of `run` pages from t run on: a multiple of four in registers, or any
+  // number that is read again each time.
   const bool all = pages <= a.most;                // (then there are no keys)
+  const bool fits = pages <= kHeldKeys * NT;
+  const int run = fits ? (pages + 4 * NT - 1) / (4 * NT) * 4 : (pages + NT - 1) / NT, mine0 = tid * run;
   auto key_at = [&](int i) -> uint32_t {
     return i >= pages ? 0u : all ? (exists(table[i]) ? kAlways : 0u) : keys[i];
   };
   uint32_t held[kHeldKeys];
-  const bool fits = pages <= kHeldKeys * NT;
 #pragma unroll
-  for (int r = 0; r < kHeldKeys; ++r) held[r] = r * NT < pages ? key_at(r * NT + tid) : 0u;
-
-  // Pages are picked whose key is above `limit`, and the first `ties` of those with that key.
+  for (int r = 0; r < kHeldKeys; r += 4) {
+    v4u k = {0u, 0u, 0u, 0u};
+    if (fits && r < run) {                         // (uniform)
+      if (!all && mine0 + r + 4 <= pages) {
+        k = *reinterpret_cast<const v4u*>(keys + mine0 + r);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = key_at(mine0 + r + u);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) held[r + u] = k[u];
+  }
+  auto each_key = [&](auto f) {
+    if (fits) {
+#pragma unroll
+      for (int r = 0; r < kHeldKeys; r += 4) {
+        if (r >= run) break;                       // (uniform)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f(held[r + u], mine0 + r + u);
+      }
+    } else {
+      for (int r = 0; r < run; ++r) f(key_at(mine0 + r), mine0 + r);
+    }
+  };
+  // Pages are picked whose key is above `limit`, and the first `ties` of those with that key.  The
+  // limit is found by counting the keys in bins of a range that holds it, which the next pass divides.
   uint32_t limit = 0u;
   int ties = 0;
   if (!all) {
-    int turn = 0;
-    auto count = [&](uint32_t least) {             // keys from `least` on
-      int c = 0;
-      if (fits) {
+    uint32_t least = kAlways, top = 0u;            // of the keys that are to be compared
+    int there = 0, always = 0;
+    each_key([&](uint32_t k, int) {
+      there += k != 0u;
+      always += k == kAlways;
+      const bool normal = k != 0u && k != kAlways;
+      least = normal ? min(least, k) : least;
+      top = normal ? max(top, k) : top;
+    });
+    there = wave_scan_sum(there);
+    always = wave_scan_sum(always);
+    least = (uint32_t)wave_scan((int)least, -1, [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
+    top = (uint32_t)wave_scan((int)top, 0, [](int x, int y) { return (int)max((uint32_t)x, (uint32_t)y); });
+    if (lane == 63) {
+      hist[0][wave] = (int)least;
+      hist[0][W + wave] = (int)top;
+      sums[1][wave] = there;
+      sums[2][wave] = always;
+    }
+    __syncthreads();
+    there = always = 0;
+    least = kAlways;
+    top = 0u;
 #pragma unroll
-        for (int r = 0; r < kHeldKeys; ++r)
-          if (r * NT < pages) c += __popcll(__builtin_amdgcn_ballot_w64(held[r] >= least));
+    for (int w = 0; w < W; ++w) {
+      there += sums[1][w];
+      always += sums[2][w];
+      least = min(least, (uint32_t)hist[0][w]);
+      top = max(top, (uint32_t)hist[0][W + w]);
+    }
+    there = __builtin_amdgcn_readfirstlane(there);
+    int need = a.most - __builtin_amdgcn_readfirstlane(always);
+    if (there > a.most) {
+      if (need == 0) {
+        limit = kAlways - 1u;
       } else {
-        for (int i = tid; i - tid < pages; i += NT)
-          c += __popcll(__builtin_amdgcn_ballot_w64(key_at(i) >= least));
-      }
-      if (lane == 0) counts[turn & 1][wave] = c;
-      __syncthreads();
-      c = 0;
+        uint32_t from = __builtin_amdgcn_readfirstlane(least);
+        int bits = 32 - __clz((int)(__builtin_amdgcn_readfirstlane(top) - from));   // of the range
+        __syncthreads();                           // (the bins are read)
+        for (int i = tid; i < 2 * kBins; i += NT) hist[0][i] = 0;
+        __syncthreads();
+        for (int turn = 0;; turn ^= 1) {
+          const int shift_by = max(bits - 10, 0);
+          const uint32_t in_range = 1u << (bits - shift_by);           // (keys behind it count no more)
+          int* bins = hist[turn];
+          each_key([&](uint32_t k, int) {
+            const uint32_t bin = (k - from) >> shift_by;
+            if (k != kAlways && k >= from && bin < in_range) atomicAdd(&bins[bin], 1);
+          });
+          __syncthreads();
+          // From the highest bin down, two a thread.
+          const int c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid];
+          static_assert(kBins == 2 * NT, "two bins a thread");
+          int incl = wave_scan_sum(c0 + c1);
+          if (lane == 63) sums[0][wave] = incl;
+          __syncthreads();
 #pragma unroll
-      for (int w = 0; w < W; ++w) c += counts[turn & 1][w];
-      ++turn;
-      return __builtin_amdgcn_readfirstlane(c);
-    };
-    if (count(1u) > a.most) {
-      // More than `most` from `lo` on, fewer from `hi` on.
-      uint64_t lo = 1, hi = (uint64_t)1 << 32;
-      int above = 0;
-      while (hi - lo > 1) {
-        const uint64_t mid = (lo + hi) / 2;
-        const int c = count((uint32_t)mid);
-        if (c == a.most) {
-          lo = mid - 1;
-          above = c;
-          break;
+          for (int w = 0; w < W; ++w) incl += w < wave ? sums[0][w] : 0;
+          const int before = incl - c0 - c1;
+          if (before < need && need <= incl) {     // (one thread)
+            const bool second = need > before + c0;
+            found[0] = kBins - 1 - 2 * tid - (second ? 1 : 0);
+            found[1] = second ? before + c0 : before;
+            found[2] = second ? c1 : c0;
+          }
+          bins[kBins - 1 - 2 * tid] = bins[kBins - 2 - 2 * tid] = 0;
+          __syncthreads();
+          from += (uint32_t)__builtin_amdgcn_readfirstlane(found[0]) << shift_by;
+          need -= __builtin_amdgcn_readfirstlane(found[1]);
+          if (need == __builtin_amdgcn_readfirstlane(found[2])) {      // all of the bin
+            limit = from - 1u;
+            break;
+          }
+          if (shift_by == 0) {
+            limit = from;
+            ties = need;
+            break;
+          }
+          bits = shift_by;
         }
-        if (c > a.most) lo = mid;
-        else hi = mid, above = c;
       }
-      limit = (uint32_t)lo;
-      ties = a.most - above;
     }
   }
 
@@ -378,59 +464,51 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
   const int first = part * a.run;                  // tiles
   const int from = (int)((int64_t)first * TT >> shift);
   const int until = (int)(((int64_t)(first + a.run) * TT + (1 << shift) - 1) >> shift);
-  int gt_before = 0, eq_before = 0;
-  for (int r0 = 0; r0 * NT < pages; r0 += kHeldKeys) {
-    uint64_t gt[kHeldKeys], eq[kHeldKeys];
-    __syncthreads();                               // (`packed` is read)
-#pragma unroll
-    for (int r = 0; r < kHeldKeys; ++r) {
-      gt[r] = eq[r] = 0;
-      if ((r0 + r) * NT < pages) {
-        const uint32_t k = r0 ? key_at((r0 + r) * NT + tid) : held[r];
-        gt[r] = __builtin_amdgcn_ballot_w64(k > limit);
-        eq[r] = ties ? __builtin_amdgcn_ballot_w64(k == limit) : 0;
-      }
-      if (lane == 0) packed[r * W + wave] = __popcll(gt[r]) << 16 | __popcll(eq[r]);
-    }
-    __syncthreads();
-    // Sums before each (r, wave): every wave adds up two entries a lane (fewer than 2^16 of either).
-    static_assert(kHeldKeys * W == 128, "two entries a lane");
-    const int x = packed[2 * lane], y = packed[2 * lane + 1];
-    int incl = x + y;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(incl, o, 64);
-      incl += lane >= o ? up : 0;
-    }
-    const int sums = __builtin_amdgcn_readlane(incl, 63), excl = incl - x - y;
-#pragma unroll
-    for (int r = 0; r < kHeldKeys; ++r) {
-      if ((r0 + r) * NT >= pages) continue;        // (uniform)
-      const int entry = r * W + wave;
-      const int b = __builtin_amdgcn_readlane(excl, entry >> 1) +
-                    (entry & 1 ? __builtin_amdgcn_readlane(x, entry >> 1) : 0);
-      const uint64_t below = ((uint64_t)1 << lane) - 1;
-      const int rank = eq_before + (b & 0xffff) + __popcll(eq[r] & below);
-      const bool tie = (eq[r] >> lane & 1) && rank < ties;
-      const int pos = gt_before + (b >> 16) + __popcll(gt[r] & below) + min(rank, ties);
-      if (((gt[r] >> lane & 1) || tie) && pos >= from && pos < until) {
-        const int i = (r0 + r) * NT + tid;
-        a.picked[(int64_t)pair * a.most + pos] = i;        // (the same by every reader of it)
-        if (pos - from < kListed) {
-          list_entry[pos - from] = i;
-          list_page[pos - from] = table[i];
-        }
-      }
-    }
-    gt_before += sums >> 16;
-    eq_before += sums & 0xffff;
+  int gt = 0, eq = 0;
+  each_key([&](uint32_t k, int) {
+    gt += k > limit;
+    eq += ties && k == limit;
+  });
+  int gt_before = wave_scan_sum(gt), eq_before = wave_scan_sum(eq);
+  if (lane == 63) {
+    sums[1][wave] = gt_before;
+    sums[2][wave] = eq_before;
   }
-  const int picked = gt_before + min(eq_before, ties);
+  __syncthreads();
+  int gt_all = 0, eq_all = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const int x = sums[1][w], y = sums[2][w];
+    gt_before += w < wave ? x : 0;
+    eq_before += w < wave ? y : 0;
+    gt_all += x;
+    eq_all += y;
+  }
+  gt_before -= gt;
+  eq_before -= eq;
+  if (gt + eq > 0)
+    each_key([&](uint32_t k, int i) {
+      const bool above = k > limit, tie = ties && k == limit;
+      const int pos = gt_before + min(eq_before, ties);
+      if ((above || (tie && eq_before < ties)) && pos >= from && pos < until) {
+        if (pos - from < kListed) list_entry[pos - from] = i;
+        else a.picked[(int64_t)pair * a.most + pos] = i;     // (the same by every reader of it)
+      }
+      gt_before += above;
+      eq_before += tie;
+    });
+  const int picked = __builtin_amdgcn_readfirstlane(gt_all) + min(__builtin_amdgcn_readfirstlane(eq_all), ties);
   const int tiles = (int)(((int64_t)picked << shift) + TT - 1) / TT;
   const int parts = max(1, (tiles + a.run - 1) / a.run);
   if (part >= parts) return;                       // (uniform)
   if (part == 0 && hgi == 0)
     for (int i = picked + tid; i < a.most; i += NT) a.picked[(int64_t)pair * a.most + i] = -1;
+  __syncthreads();
+  for (int j = tid; j < min(min(until, picked) - from, kListed); j += NT) {
+    const int i = list_entry[j];
+    list_page[j] = table[i];
+    a.picked[(int64_t)pair * a.most + from + j] = i;
+  }
   __syncthreads();
 
   // Attention over the picked pages' tokens, as if they were one sequence: token v of it.
@@ -586,6 +664,9 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
   if (tid == 0) *counter = 0u;                     // as the next call expects it
 }
 
+// Rows of keys begin at 16 bytes.
+int64_t key_stride_of(int64_t max_pages) { return (max_pages + 3) / 4 * 4; }
+
 // Rows, and part slots: rows that are shared are so by no more workgroups than fill the chip.
 int64_t sparse_rows(int64_t batch, int n_q_heads, int n_kv_heads) {
   const int G = n_q_heads / n_kv_heads;
@@ -617,14 +698,14 @@ aatc_status launch_bounds(const BoundsArgs& a, aatc_dtype dtype, void* stream) {
 
 size_t sparse_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int64_t max_pages) {
   return kSparseCountersBytes + round256(sparse_parts_bytes(slot_heads_of(n_q_heads, n_kv_heads))) +
-         (size_t)batch * n_kv_heads * max_pages * sizeof(uint32_t);
+         (size_t)batch * n_kv_heads * key_stride_of(max_pages) * sizeof(uint32_t);
 }
 
 bool sparse_fits(int64_t batch, int n_q_heads, int n_kv_heads, int64_t max_pages) {
   if (n_q_heads / n_kv_heads > kMaxSay) return false;
   const int64_t pairs = batch * n_kv_heads;
   if (max_pages > ((int64_t)1 << 30) / pairs) return false;
-  return pairs * ((max_pages + kChunk - 1) / kChunk) <= kMaxSparseGroups &&
+  return pairs * ((max_pages + 63) / 64) <= kMaxSparseGroups &&
          sparse_rows(batch, n_q_heads, n_kv_heads) <= kMaxSparseGroups;
 }
 
@@ -637,21 +718,29 @@ aatc_status launch_sparse(SparseArgs a, aatc_dtype c_dtype, void* workspace, voi
   p.parts = reinterpret_cast<Partial*>(parts);
   p.parts_bytes = (int)sparse_parts_bytes(p.slot_heads);
   a.keys = reinterpret_cast<uint32_t*>(parts + round256(p.parts_bytes));
+  a.key_stride = key_stride_of(p.max_pages);
   const int tt = c_dtype == AATC_F32 ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   const int64_t rows = sparse_rows(p.batch, p.n_q_heads, p.n_kv_heads);
   const int64_t tokens = (int64_t)std::min(a.most, p.max_pages) << p.page_shift;
   const int tiles = (int)((tokens + tt - 1) / tt);
-  // Rows are shared where there are fewer than workgroups, two tiles a wave at least.
+  // Rows are shared where there are fewer than workgroups, a tile a wave at least.
   const int share = rows < kSparseGroups ? kSparseGroups / (int)rows : 1;
-  a.run = std::max((tiles + share - 1) / share, std::min(tiles, 2 * kSparseWaves));
+  a.run = std::max((tiles + share - 1) / share, std::min(tiles, kSparseWaves));
   a.parts = (tiles + a.run - 1) / a.run;
   const hipStream_t st = (hipStream_t)stream;
   if (p.max_pages > a.most) {                      // (else every page is picked)
-    const int64_t groups = (int64_t)p.batch * p.n_kv_heads * ((p.max_pages + kChunk - 1) / kChunk);
-    if (p.hg == 1)
-      hipLaunchKernelGGL(score_kernel<true>, dim3((unsigned)groups), dim3(256), 0, st, a);
+    // Few pages in small chunks, for the chip's sake; many in large ones, whose queries' codes count less.
+    const int64_t pairs = (int64_t)p.batch * p.n_kv_heads;
+    const bool many = pairs * p.max_pages >= 256 * 1024;
+    const int chunk = many ? 256 : 64;
+    const dim3 groups((unsigned)(pairs * ((p.max_pages + chunk - 1) / chunk)));
+    if (p.hg > 1)
+      hipLaunchKernelGGL((score_kernel<false, 4>), dim3((unsigned)(pairs * ((p.max_pages + 255) / 256))),
+                         dim3(256), 0, st, a);
+    else if (many)
+      hipLaunchKernelGGL((score_kernel<true, 4>), groups, dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL(score_kernel<false>, dim3((unsigned)groups), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((score_kernel<true, 1>), groups, dim3(256), 0, st, a);
     if (hipGetLastError() != hipSuccess) return AATC_E_DEVICE;
   }
   auto launch = [&](auto kernel) {
