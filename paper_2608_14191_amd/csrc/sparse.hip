@@ -50,15 +50,101 @@ __device__ inline float power_of_two(int e) {     // -126 <= e <= 127
 
 // --- bounds ---------------------------------------------------------------------------------------
 
-// A wave takes a page of a KV head at a time: a row of 16 (32 in float32) lanes has a token, a lane 16
-// bytes of it; what the rows have meets in row swaps.  Reads every key once: the memory bounds it.
+// A wave takes a run of (page, KV head) pairs, one at a time: a row of 16 (32 in float32) lanes has a
+// token, a lane 16 bytes of it; what the rows have meets in row swaps.  Reads every key once, past the
+// caches: the memory bounds it (65536 tokens x 8 float32 heads: 5.9 TB/s), small pages the vector units.
+// 16-bit values are compared as whole numbers in their order, two at a time.
 constexpr int kBoundWaves = 4, kBoundGroups = 2048;
+
+// Largest and smallest of what a lane has seen, channel by channel.
+template <class T>
+struct Extremes {                                  // 16 bits: eight channels, in pairs
+  typedef int16_t v2 __attribute__((ext_vector_type(2)));
+  static constexpr int N = 8;
+  // The number that is larger the larger the value is (its own inverse); infinities and NaN lie at
+  // either end.
+  static constexpr int kInfinite = __is_same(T, _Float16) ? 0x7c00 : 0x7f80;
+  v2 top[4], low[4];
+  __device__ void clear() {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) top[d] = (v2){-32768, -32768}, low[d] = (v2){32767, 32767};
+  }
+  static __device__ v2 pair(uint32_t x) { return __builtin_bit_cast(v2, x); }
+  static __device__ uint32_t word(v2 x) { return __builtin_bit_cast(uint32_t, x); }
+  __device__ void add(v4u x) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      v2 v = pair(x[d]);
+      v ^= (v >> 15) & (v2){0x7fff, 0x7fff};
+      top[d] = __builtin_elementwise_max(top[d], v);
+      low[d] = __builtin_elementwise_min(low[d], v);
+    }
+  }
+  __device__ void join_rows() {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      auto r = __builtin_amdgcn_permlane16_swap(word(top[d]), word(top[d]), false, false);
+      top[d] = __builtin_elementwise_max(pair(r[0]), pair(r[1]));
+      r = __builtin_amdgcn_permlane32_swap(word(top[d]), word(top[d]), false, false);
+      top[d] = __builtin_elementwise_max(pair(r[0]), pair(r[1]));
+      r = __builtin_amdgcn_permlane16_swap(word(low[d]), word(low[d]), false, false);
+      low[d] = __builtin_elementwise_min(pair(r[0]), pair(r[1]));
+      r = __builtin_amdgcn_permlane32_swap(word(low[d]), word(low[d]), false, false);
+      low[d] = __builtin_elementwise_min(pair(r[0]), pair(r[1]));
+    }
+  }
+  static __device__ float value(int16_t x) {
+    const uint16_t bits = (uint16_t)(x ^ ((x >> 15) & 0x7fff));
+    return (float)__builtin_bit_cast(T, bits);
+  }
+  __device__ float largest(int i) const { return value(top[i / 2][i % 2]); }
+  __device__ float smallest(int i) const { return value(low[i / 2][i % 2]); }
+  __device__ bool bad() const {
+    bool b = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) b |= (top[i / 2][i % 2] >= kInfinite) | (low[i / 2][i % 2] <= ~kInfinite);
+    return b;
+  }
+};
+template <>
+struct Extremes<float> {
+  static constexpr int N = 4;
+  float top[4], low[4];
+  bool odd;
+  __device__ void clear() {
+    odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top[i] = -INFINITY, low[i] = INFINITY;
+  }
+  __device__ void add(v4u x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = __uint_as_float(x[i]);
+      odd |= !(fabsf(v) < INFINITY);
+      top[i] = fmaxf(top[i], v);
+      low[i] = fminf(low[i], v);
+    }
+  }
+  __device__ void join_rows() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[i]), __float_as_uint(top[i]), false, false);
+      top[i] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+      r = __builtin_amdgcn_permlane32_swap(__float_as_uint(low[i]), __float_as_uint(low[i]), false, false);
+      low[i] = fminf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+  }
+  __device__ float largest(int i) const { return top[i]; }
+  __device__ float smallest(int i) const { return low[i]; }
+  __device__ bool bad() const { return odd; }
+};
 
 template <class T>
 __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) {
-  constexpr int NT = 64 * kBoundWaves;
-  constexpr int N = 16 / sizeof(T), L = kD / N;    // channels of a lane, lanes of a token
-  __shared__ int before[NT];                       // pages of the threads' rows before
+  constexpr int W = kBoundWaves, NT = 64 * W;
+  constexpr int N = Extremes<T>::N, L = kD / N;    // channels of a lane, lanes of a token
+  constexpr int U = 16 / (64 / L);                 // loads of 16 tokens
+  __shared__ int before[NT], sums[W];              // pages of the threads' rows up to their last
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int each = (a.rows + NT - 1) / NT;
@@ -71,86 +157,95 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
   };
   int mine = 0, skip;
   for (int b = min(tid * each, a.rows); b < min((tid + 1) * each, a.rows); ++b) mine += pages_of(b, skip);
-  before[tid] = mine;
+  int incl = wave_scan_sum(mine);                  // (pages of all rows: below 2^30)
+  if (lane == 63) sums[wave] = incl;
   __syncthreads();
+  int total = 0;
 #pragma unroll
-  for (int o = 1; o < NT; o <<= 1) {               // (pages of all rows: below 2^30)
-    const int x = tid >= o ? before[tid - o] : 0;
-    __syncthreads();
-    before[tid] += x;
-    __syncthreads();
+  for (int w = 0; w < W; ++w) {
+    incl += w < wave ? sums[w] : 0;
+    total += sums[w];
   }
-  const int total = before[NT - 1];
-  const int64_t items = (int64_t)total * a.n_kv_heads;
-  for (int64_t item = (int64_t)blockIdx.x * kBoundWaves + wave; item < items;
-       item += (int64_t)gridDim.x * kBoundWaves) {
-    const int at = (int)(item / a.n_kv_heads), head = (int)(item - (int64_t)at * a.n_kv_heads);
-    // The row: the first thread whose sum passes `at`, then its rows in turn.
-    int lo = 0, hi = NT - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (before[mid] > at) hi = mid;
-      else lo = mid + 1;
-    }
-    int left = at - (lo ? before[lo - 1] : 0), b = lo * each, first, n;
-    while (n = pages_of(b, first), left >= n) left -= n, ++b;
+  before[tid] = incl;
+  __syncthreads();
+  // This wave's run of pairs, the heads of a page one after another.
+  const int64_t items = (int64_t)__builtin_amdgcn_readfirstlane(total) * a.n_kv_heads;
+  const int64_t waves = (int64_t)gridDim.x * W, me = (int64_t)blockIdx.x * W + wave;
+  const int begin = (int)(items * me / waves), end = (int)(items * (me + 1) / waves);
+  if (begin >= end) return;
+  int at = begin / a.n_kv_heads, head = begin - at * a.n_kv_heads;
+  // Its row: the first thread whose sum passes `at`, then that thread's rows in turn.
+  int lo = 0, hi = NT - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (before[mid] > at) hi = mid;
+    else lo = mid + 1;
+  }
+  int left = at - (lo ? before[lo - 1] : 0), b = lo * each, first, n;
+  while (n = pages_of(b, first), left >= n) left -= n, ++b;
+  for (int item = begin;;) {
     const int entry = first + left;
-    const int page = a.table[b * a.table_stride + entry];
-    if (page < 0 || page >= a.n_pages) continue;   // (uniform)
+    const int page = __builtin_amdgcn_readfirstlane(a.table[b * a.table_stride + entry]);
     const int held = min(tokens(a.wanted, b) - (entry << a.page_shift), 1 << a.page_shift);
-    const char* src = a.k + page * a.page_stride + head * a.head_stride + 16 * (lane % L);
-    float top[N], low[N];
-    bool bad = false;
+    const bool there = page >= 0 && page < a.n_pages;        // (uniform)
+    if (there) {
+      const char* src = a.k + page * a.page_stride + head * a.head_stride + 16 * (lane % L);
+      Extremes<T> x;
+      x.clear();
+      for (int t = lane / L; t < held; t += U * (64 / L)) {
+        v4u v[U];
 #pragma unroll
-    for (int i = 0; i < N; ++i) top[i] = -INFINITY, low[i] = INFINITY;
-    constexpr int U = 4;                           // tokens of a lane in flight
-    for (int t = lane / L; t < held; t += U * (64 / L)) {
-      v4u x[U];
+        for (int u = 0; u < U; ++u)                // (a token twice does no harm)
+          v[u] = __builtin_nontemporal_load(
+              reinterpret_cast<const v4u*>(src + min(t + u * (64 / L), held - 1) * a.tok_stride));
 #pragma unroll
-      for (int u = 0; u < U; ++u)                  // (a token twice does no harm)
-        x[u] = *reinterpret_cast<const v4u*>(src + min(t + u * (64 / L), held - 1) * a.tok_stride);
+        for (int u = 0; u < U; ++u) x.add(v[u]);
+      }
+      const bool none = __builtin_amdgcn_ballot_w64(x.bad() && lane / L < held) != 0;
+      x.join_rows();
+      float most = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        T e[N];
-        __builtin_memcpy(e, &x[u], 16);
+      for (int i = 0; i < N; ++i) most = fmaxf(most, fmaxf(fabsf(x.largest(i)), fabsf(x.smallest(i))));
+      // (over the lanes of a token: rotations within rows of 16, and a swap of two rows)
+      auto over = [&](auto ctrl) {
+        most = fmaxf(most, __uint_as_float(__builtin_amdgcn_update_dpp(
+                               0, (int)__float_as_uint(most), decltype(ctrl)::value, 0xf, 0xf, true)));
+      };
+      over(std::integral_constant<int, 0x128>{});
+      over(std::integral_constant<int, 0x124>{});
+      over(std::integral_constant<int, 0x122>{});
+      over(std::integral_constant<int, 0x121>{});
+      if constexpr (L == 32) {
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        most = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+      }
+      const int e = step_of(none ? 0.f : most);
+      const bool wide = none || e > kHighestStep;
+      const float up = power_of_two(wide ? 0 : -e);
+      // The first row of lanes stores the upper bounds, the second the lower ones.
+      if (lane < 2 * L) {
+        const bool upper = lane < L;
+        int8_t code[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float v = (float)e[i];
-          bad |= !(fabsf(v) < INFINITY);
-          top[i] = fmaxf(top[i], v);
-          low[i] = fminf(low[i], v);
+          // (a product that falls below the smallest number still rounds away from 0)
+          const float v = upper ? x.largest(i) : -x.smallest(i);
+          const float c = v > 0.f ? fmaxf(ceilf(v * up), 1.f) : ceilf(v * up);
+          code[i] = wide ? 0 : (int8_t)(upper ? c : -c);
         }
+        const int64_t to = (int64_t)page * a.n_kv_heads + head;
+        __builtin_memcpy(a.codes + to * kBoundBytes + (upper ? 0 : kD) + N * (lane % L), code, N);
+        if (lane == 0) a.scales[to] = wide ? INFINITY : power_of_two(e);
       }
     }
-    float most = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-#pragma unroll
-      for (int o = L; o < 64; o <<= 1) {
-        top[i] = fmaxf(top[i], __shfl_xor(top[i], o, 64));
-        low[i] = fminf(low[i], __shfl_xor(low[i], o, 64));
+    if (++item == end) return;
+    if (++head == a.n_kv_heads) {
+      head = 0;
+      if (++left == n) {
+        left = 0;
+        do n = pages_of(++b, first);               // (there are items left: some row has them)
+        while (n == 0);
       }
-      most = fmaxf(most, fmaxf(fabsf(top[i]), fabsf(low[i])));
-    }
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-    const int e = step_of(most);
-    const bool none = __builtin_amdgcn_ballot_w64(bad) != 0 || e > kHighestStep;
-    const float up = power_of_two(none ? 0 : -e);
-    // The first row of lanes stores the upper bounds, the second the lower ones.
-    if (lane < 2 * L) {
-      const bool upper = lane < L;
-      int8_t code[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        // (a product that falls below the smallest number still rounds away from 0)
-        const float c = upper ? top[i] > 0.f ? fmaxf(ceilf(top[i] * up), 1.f) : ceilf(top[i] * up)
-                              : low[i] < 0.f ? fminf(floorf(low[i] * up), -1.f) : floorf(low[i] * up);
-        code[i] = none ? 0 : (int8_t)c;
-      }
-      const int64_t to = (int64_t)page * a.n_kv_heads + head;
-      __builtin_memcpy(a.codes + to * kBoundBytes + (upper ? 0 : kD) + N * (lane % L), code, N);
-      if (lane == 0) a.scales[to] = none ? INFINITY : power_of_two(e);
     }
   }
 }
