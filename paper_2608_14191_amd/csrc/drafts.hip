@@ -11,8 +11,8 @@
 //   itself, keys and values go from memory to its registers;
 //   more, bound by the matrix cores (P in two or three terms: 1.5 or 2 products for one of a plain
 //   attention) and the vector units (exponentials, splitting) about alike: the waves of a workgroup
-//   share the tiles of a stage in LDS, each with up to 48 of its columns, so that a compute unit reads
-//   keys and values once for up to 256 columns.
+//   share the tiles of a stage in LDS, each with 16 or 32 of its columns, so that a compute unit reads
+//   keys and values once for up to 128 columns.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -29,12 +29,12 @@ namespace {
 // One workgroup a compute unit, so that a row has few parts to join.
 constexpr int kTreeGroups = 256;
 constexpr int kGroup = 16;                        // columns of a group
-constexpr int kMostCols = 256;                    // of a workgroup
+constexpr int kMostCols = 128;                    // of a workgroup
 // The workspace: part slots.  At most twice as many runs as fill the chip belong to shared rows.
 constexpr int kTreeSlots = 2 * kTreeGroups;
-// Runs are a multiple of so many tiles, twice that at least: a tile a wave for the narrow kernel, a
-// stage for the wide one.
-constexpr int kNarrowQuantum = 8, kWideQuantum = 2;
+// Runs are a multiple of so many tiles, twice that at least: what a workgroup computes in about the time
+// that the join takes.
+constexpr int quantum_of(int cols) { return cols <= 64 ? 8 : 4; }
 // The maximum that weights refer to is renewed when a score passes it by this much (exponents of 2):
 // sums and outputs are rescaled rarely.  Weights of 2^(slack + below) have to fit their type, and in
 // f16 small ones stay off the denormals.
@@ -226,11 +226,15 @@ struct TreePages {
 };
 
 // What a wave has of C groups of columns, from column col0 of the workgroup's block on: running
-// maxima (exponents of 2), sums and value sums (acc[c][j][i]: channel M::channel(j, i, g) of column
+// maxima (exponents of 2), sums and value sums (acc[c][j][i]: channel channel(j, i, g) of column
 // 16 c + n).
-template <class M, int QT, int C>
+// TURNED: values come turned from LDS (product j then has other channels).
+template <class M, int QT, int C, bool TURNED>
 struct TreeWave {
   using Tile = M;
+  static __device__ int channel(int j, int i, int g) {
+    return TURNED ? M::turned_channel(j, i, g) : M::channel(j, i, g);
+  }
   static constexpr int TT = M::kTokens, NM = M::kMine;
   const PagedArgs& p;
   const TreeInfo& info;
@@ -272,13 +276,12 @@ struct TreeWave {
            __builtin_amdgcn_ballot_w64(!there) == 0;
   }
 
+  // Whether any column may attend token t, if its page exists.
+  __device__ bool counts(int t) const { return (t < end) & ((t >= lo) | (t < p.sink)); }
   // Tokens that no column attends become zeros; returns which others are not finite (bit e).
   __device__ unsigned mask_values(int t0, bool there, typename M::Values& val) const {
 #pragma unroll
-    for (int e = 0; e < NM; ++e) {
-      const int t = t0 + NM * g + e;
-      val.keep(e, there & (t < end) & ((t >= lo) | (t < p.sink)));
-    }
+    for (int e = 0; e < NM; ++e) val.keep(e, there & counts(t0 + NM * g + e));
     unsigned dirty = 0u;
     if (__builtin_amdgcn_ballot_w64(M::any_bad(val)))
 #pragma unroll
@@ -339,6 +342,27 @@ struct TreeWave {
     typename M::Turned turned;
     M::turn(val, turned);
     next_values();
+    weigh_and_add(t0, whole, there, key, turned, next_keys);
+  }
+  __device__ void step(int t0, bool there, const typename M::Keys& key, typename M::Turned& turned) {
+    const bool whole = is_whole(t0, there);
+    if (!whole) {
+      unsigned on = 0u;
+#pragma unroll
+      for (int e = 0; e < NM; ++e) on |= there & counts(t0 + NM * g + e) ? 1u << e : 0u;
+      M::keep_turned(turned, on);
+      if (__builtin_amdgcn_ballot_w64(M::any_bad(turned))) {
+        odd = true;                                // (these values: odd_values)
+        M::drop_bad(turned);
+      }
+    }
+    weigh_and_add(t0, whole, there, key, turned, [] {});
+  }
+
+  template <class K>
+  __device__ __forceinline__ void weigh_and_add(int t0, bool whole, bool there,
+                                                const typename M::Keys& key,
+                                                const typename M::Turned& turned, K next_keys) {
     float z[C][NM];
 #pragma unroll
     for (int c = 0; c < C; ++c) M::template scores<QT>(key, q[c], z[c]);
@@ -411,20 +435,33 @@ struct TreeWave {
       for (int tok = 0; tok < TT; ++tok) {
         const int ge = tok / NM, te = tok % NM;
         if (!__builtin_amdgcn_ballot_w64(g == ge && (dirty >> te & 1u))) continue;
-        typename M::Values one = val;              // the token's row, in place of the first
-        float w[NM];
+        float w[NM];                               // the token in place of the first
         w[0] = z[0];
 #pragma unroll
         for (int e = 1; e < NM; ++e) {
-          M::take(one, val, e, e == te);
-          one.keep(e, false);
           w[0] = e == te ? z[e] : w[0];
           w[e] = 0.f;
         }
-        one.keep(0, g == ge);
         w[0] = __builtin_amdgcn_exp2f(w[0] - ref);
         typename M::Turned turned;
-        M::turn(one, turned);
+        if constexpr (TURNED) {
+          const int t = t0 + tok, page = pages.page_of(t);
+          const char* row = p.v + pages.slot_of(t, page) + 2 * n;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t v = *reinterpret_cast<const uint16_t*>(row + 32 * j);
+            turned.a[j] = (v4u){g == ge && M::bad16(v) ? v : 0u, 0u, 0u, 0u};   // (the others are in)
+          }
+        } else {
+          typename M::Values one = val;
+#pragma unroll
+          for (int e = 1; e < NM; ++e) {
+            M::take(one, val, e, e == te);
+            one.keep(e, false);
+          }
+          one.keep(0, g == ge);
+          M::turn(one, turned);
+        }
         const bool on = __shfl(bits, n + 16 * ge, 64) >> te & 1u;
         const auto terms = M::split(w);
 #pragma unroll
@@ -473,7 +510,6 @@ __device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, 
                                            TreeSpace<W>& sh, Wave& x, Sums sums,
                                            std::integral_constant<int, C>) {
   constexpr int NT = 64 * W, CW = W / TW;
-  using M = typename Wave::Tile;
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -494,7 +530,7 @@ __device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, 
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mine[M::channel(j, i, g)] = x.acc[c][j][i];
+      for (int i = 0; i < 4; ++i) mine[Wave::channel(j, i, g)] = x.acc[c][j][i];
     __syncthreads();
     for (int y = tid; y < CW * kGroup * (kD / 4); y += NT) {
       const int h = y / (kD / 4) % kGroup, c4 = y % (kD / 4), w0 = y / (kGroup * (kD / 4)) * TW;
@@ -526,7 +562,7 @@ __device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, 
 
 // The parts of the rows that are shared, joined in their order: the same grid as the runs', and as many
 // workgroups as a row has parts take a share of its columns each.  (A join by the last of a row's
-// workgroups would read up to 4 MiB alone: 100 us at 32 parts of 256 columns.)
+// workgroups would read up to 4 MiB alone: 32 parts of 256 columns took 100 us.)
 constexpr int kJoinWaves = 8;
 
 template <int TT>
@@ -629,7 +665,7 @@ __global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
     load_keys(t0, key_page(t0));
     load_values(t0, vp);
   }
-  TreeWave<M, QT, 1> x(a, r, sh.info, 0, 0, columns);
+  TreeWave<M, QT, 1, false> x(a, r, sh.info, 0, 0, columns);
   if (wave == W - 1) find_families(a, r, sh.info);
   __syncthreads();
   for (int i = begin; i < last; i += W) {
@@ -666,26 +702,10 @@ __device__ inline void wait_loads() {
 // The keys and values of a tile in LDS.  (In assembly, with the wait: the compiler would wait for the
 // loads of the next stage too, which go elsewhere in the same array.)
 template <class M>
-__device__ inline void read_keys(typename M::Keys& to, uint32_t even, uint32_t odd) {
+__device__ inline void read_keys(typename M::Keys& to, uint32_t at) {
   v4u x[8];
   static_assert(sizeof to == sizeof x, "eight pieces");
-  asm volatile(
-      "ds_read_b128 %0, %8 offset:%10\n\tds_read_b128 %1, %9 offset:%11\n\t"
-      "ds_read_b128 %2, %8 offset:%12\n\tds_read_b128 %3, %9 offset:%13\n\t"
-      "ds_read_b128 %4, %8 offset:%14\n\tds_read_b128 %5, %9 offset:%15\n\t"
-      "ds_read_b128 %6, %8 offset:%16\n\tds_read_b128 %7, %9 offset:%17\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
-        "=&v"(x[7])
-      : "v"(even), "v"(odd), "n"(M::key_offset(0)), "n"(M::key_offset(1)), "n"(M::key_offset(2)),
-        "n"(M::key_offset(3)), "n"(M::key_offset(4)), "n"(M::key_offset(5)), "n"(M::key_offset(6)),
-        "n"(M::key_offset(7))
-      : "memory");
-  __builtin_memcpy(&to, x, sizeof x);
-}
-template <class M>
-__device__ inline void read_values(typename M::Values& to, const uint32_t (&at)[4]) {
-  v4u x[8];
-  static_assert(sizeof to == sizeof x, "eight pieces");
+  const uint32_t p[4] = {at, at ^ 64u, at ^ 128u, at ^ 192u};
   asm volatile(
       "ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%17\n\t"
       "ds_read_b128 %2, %10 offset:%18\n\tds_read_b128 %3, %11 offset:%19\n\t"
@@ -693,15 +713,59 @@ __device__ inline void read_values(typename M::Values& to, const uint32_t (&at)[
       "ds_read_b128 %6, %14 offset:%22\n\tds_read_b128 %7, %15 offset:%23\n\ts_waitcnt lgkmcnt(0)"
       : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
         "=&v"(x[7])
-      : "v"(at[M::value_turn(0)]), "v"(at[M::value_turn(1)]), "v"(at[M::value_turn(2)]),
-        "v"(at[M::value_turn(3)]), "v"(at[M::value_turn(4)]), "v"(at[M::value_turn(5)]),
-        "v"(at[M::value_turn(6)]), "v"(at[M::value_turn(7)]), "n"(kHalfStage + M::value_offset(0)),
+      : "v"(p[M::key_flip(0)]), "v"(p[M::key_flip(1)]), "v"(p[M::key_flip(2)]),
+        "v"(p[M::key_flip(3)]), "v"(p[M::key_flip(4)]), "v"(p[M::key_flip(5)]),
+        "v"(p[M::key_flip(6)]), "v"(p[M::key_flip(7)]), "n"(M::key_offset(0)),
+        "n"(M::key_offset(1)), "n"(M::key_offset(2)), "n"(M::key_offset(3)), "n"(M::key_offset(4)),
+        "n"(M::key_offset(5)), "n"(M::key_offset(6)), "n"(M::key_offset(7))
+      : "memory");
+  __builtin_memcpy(&to, x, sizeof x);
+}
+template <class M>
+__device__ inline void read_values(typename M::Values& to, uint32_t at) {
+  v4u x[8];
+  static_assert(sizeof to == sizeof x, "eight pieces");
+  const uint32_t p[4] = {at, at ^ 16u, at ^ 32u, at ^ 48u};
+  asm volatile(
+      "ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%17\n\t"
+      "ds_read_b128 %2, %10 offset:%18\n\tds_read_b128 %3, %11 offset:%19\n\t"
+      "ds_read_b128 %4, %12 offset:%20\n\tds_read_b128 %5, %13 offset:%21\n\t"
+      "ds_read_b128 %6, %14 offset:%22\n\tds_read_b128 %7, %15 offset:%23\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+        "=&v"(x[7])
+      : "v"(p[M::value_flip(0)]), "v"(p[M::value_flip(1)]), "v"(p[M::value_flip(2)]),
+        "v"(p[M::value_flip(3)]), "v"(p[M::value_flip(4)]), "v"(p[M::value_flip(5)]),
+        "v"(p[M::value_flip(6)]), "v"(p[M::value_flip(7)]), "n"(kHalfStage + M::value_offset(0)),
         "n"(kHalfStage + M::value_offset(1)), "n"(kHalfStage + M::value_offset(2)),
         "n"(kHalfStage + M::value_offset(3)), "n"(kHalfStage + M::value_offset(4)),
         "n"(kHalfStage + M::value_offset(5)), "n"(kHalfStage + M::value_offset(6)),
         "n"(kHalfStage + M::value_offset(7))
       : "memory");
   __builtin_memcpy(&to, x, sizeof x);
+}
+template <class M>
+__device__ inline void read_turned(typename M::Turned& to, uint32_t at) {
+  typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+  v2u x[8][2];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %16 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %2, %17 offset:%24\n\tds_read_b64_tr_b16 %3, %17 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %4, %18 offset:%24\n\tds_read_b64_tr_b16 %5, %18 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %6, %19 offset:%24\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %20 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %10, %21 offset:%24\n\tds_read_b64_tr_b16 %11, %21 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %12, %22 offset:%24\n\tds_read_b64_tr_b16 %13, %22 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %14, %23 offset:%24\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]),
+        "=&v"(x[2][1]), "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]),
+        "=&v"(x[5][0]), "=&v"(x[5][1]), "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]),
+        "=&v"(x[7][1])
+      : "v"(at), "v"(at ^ 32u), "v"(at ^ 64u), "v"(at ^ 96u), "v"(at ^ 128u), "v"(at ^ 160u),
+        "v"(at ^ 192u), "v"(at ^ 224u), "n"(kHalfStage), "n"(kHalfStage + 4 * M::kRow)
+      : "memory");
+#pragma unroll
+  for (int j = 0; j < 8; ++j) to.a[j] = (v4u){x[j][0][0], x[j][0][1], x[j][1][0], x[j][1][1]};
 }
 
 template <class M, int QT, int C, int CW, int W>
@@ -732,11 +796,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
   // as many loads, so that they can be counted; behind the last tile it is that one again.)
   const int tile = wave * PT / TT, within = wave * PT % TT;
   const auto row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)pages.row;
-  int page[PT / 8];
   auto token_of = [&](int s) {
     return r.rt.token(min(r.first + s * kStage + tile, r.last - 1), TT) + within;
   };
-  auto fetch_pages = [&](int s) {
+  auto fetch_pages = [&](int s, int(&page)[PT / 8]) {
     const int t = token_of(s);
 #pragma unroll
     for (int b = 0; b < PT / 8; ++b) {
@@ -745,7 +808,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
     }
   };
   constexpr int kLoads = 2 * PT / kPer;            // of a stage, of a wave
-  auto issue = [&](int s) {
+  auto issue = [&](int s, const int(&page)[PT / 8]) {
     const int t = token_of(s), slot = s % kRing;
 #pragma unroll
     for (int i = 0; i < PT / kPer; ++i) {
@@ -767,20 +830,18 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
   };
 
   const int stages = (r.last - r.first + kStage - 1) / kStage;
-#pragma unroll 1
-  for (int s = 0; s < kRing - 1; ++s) {
-    fetch_pages(s);
-    issue(s);
-  }
-  fetch_pages(kRing - 1);
+  int page[kRing][PT / 8];
+#pragma unroll
+  for (int s = 0; s < kRing; ++s) fetch_pages(s, page[s]);
+#pragma unroll
+  for (int s = 0; s < kRing - 1; ++s) issue(s, page[s]);
   const int cw = wave / TW, tw = wave % TW;
-  TreeWave<M, QT, C> x(a, r, sh.info, cb, cw * C * kGroup, columns);
+  TreeWave<M, QT, C, M::kReadsTurned> x(a, r, sh.info, cb, cw * C * kGroup, columns);
   if (wave == W - 1) find_families(a, r, sh.info);
   const bool busy = cw * C * kGroup < columns;     // (uniform)
-  // Where the lane's pieces of a tile are (the ring is aligned to more than a row: the turns of the
-  // value pieces flip bits 4 and 5 of the address).
-  const uint32_t key0 = M::key_place(0, n, g), key1 = M::key_place(1, n, g);
-  const uint32_t value0 = M::value_place(0, n, g);
+  // Where the lane's pieces of a tile are (a ring aligned to more than a row: pieces differ in bits of
+  // the address).
+  const uint32_t key0 = M::key_place(n, g), value0 = M::value_place(n, g);
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
 #pragma unroll 1
   for (int s = 0; s < stages; ++s) {
@@ -788,8 +849,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();                  // everyone's has, and the stage before is read
     asm volatile("" ::: "memory");
-    issue(s + kRing - 1);
-    fetch_pages(s + kRing);
+    issue(s + kRing - 1, page[kRing - 1]);
+    fetch_pages(s + kRing, page[kRing - 1]);
     const int slot = s % kRing;
     if (busy)
 #pragma unroll 1
@@ -797,13 +858,19 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
         const int i = r.first + s * kStage + k;
         if (i >= r.last) break;                    // (uniform)
         typename M::Keys key;
-        typename M::Values val;
         const uint32_t from = base + slot * (2 * kHalfStage) + k * (TT * kRow);
-        const uint32_t value_at[4] = {from + value0, (from + value0) ^ 16u, (from + value0) ^ 32u,
-                                      (from + value0) ^ 48u};
-        read_keys<M>(key, from + key0, from + key1);
-        read_values<M>(val, value_at);
-        x.step(r.rt.token(i, TT), there[slot][k * TT / 8 + M::value_block(g)] != 0, key, val, [] {}, [] {});
+        read_keys<M>(key, from + key0);
+        const int t0 = r.rt.token(i, TT);
+        const bool on = there[slot][k * TT / 8 + M::value_block(g)] != 0;
+        if constexpr (M::kReadsTurned) {
+          typename M::Turned turned;
+          read_turned<M>(turned, from + value0);
+          x.step(t0, on, key, turned);
+        } else {
+          typename M::Values val;
+          read_values<M>(val, from + value0);
+          x.step(t0, on, key, val, [] {}, [] {});
+        }
       }
   }
   wait_loads<0>();                                 // (the loads behind the last stage)
@@ -815,18 +882,18 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
 }
 
 // A (sequence, KV head)'s columns in blocks of nearly as many groups each; a block's groups are dealt
-// to `cw` sets of waves, c groups each.  `most`: groups of a block.  Sixteen where two waves a SIMD have
-// room for two groups each (queries of one 16-bit term), else eight.
+// to `cw` sets of waves, c groups each.  (Blocks of 256 columns, which read keys and values half as
+// often but have twice the parts to join, took as long for 64 drafts of 32768 tokens and longer for
+// fewer tokens: 28.3 us at 1000 tokens, 33.7.)
 struct Blocks {
   int blocks, c, cw;
   int cols() const { return c * cw * kGroup; }
 };
-constexpr int kMostSame = 16, kMostOther = 8;
-Blocks blocks_of(int drafts, int G, int most) {
+Blocks blocks_of(int drafts, int G) {
   const int groups = (drafts * G + kGroup - 1) / kGroup;
   if (groups == 1) return {1, 1, 1};
-  const int blocks = (groups + most - 1) / most, each = (groups + blocks - 1) / blocks;
-  return {blocks, each <= 4 ? 1 : 2, each <= 8 ? 4 : 8};
+  const int blocks = (groups + 7) / 8, each = (groups + blocks - 1) / blocks;
+  return {blocks, each <= 4 ? 1 : 2, 4};
 }
 int units_of(int blocks) { return std::max(1, kTreeGroups / blocks); }
 
@@ -838,27 +905,24 @@ size_t tree_parts_bytes(const Blocks& b, int64_t rows) {
 }  // namespace
 
 size_t tree_workspace_bytes(int batch, int drafts, int n_q_heads, int n_kv_heads) {
-  const int G = n_q_heads / n_kv_heads;
-  const int64_t rows = (int64_t)batch * n_kv_heads;
-  return std::max(tree_parts_bytes(blocks_of(drafts, G, kMostSame), rows),
-                  tree_parts_bytes(blocks_of(drafts, G, kMostOther), rows));
+  return tree_parts_bytes(blocks_of(drafts, n_q_heads / n_kv_heads), (int64_t)batch * n_kv_heads);
 }
 
 bool tree_fits(int64_t batch, int drafts, int n_q_heads, int n_kv_heads) {
   const int64_t columns = (int64_t)drafts * (n_q_heads / n_kv_heads);
   if (columns > kMaxColumns) return false;
-  const Blocks b = blocks_of(drafts, n_q_heads / n_kv_heads, kMostOther);
+  const Blocks b = blocks_of(drafts, n_q_heads / n_kv_heads);
   return (batch * n_kv_heads + kTreeGroups + 8) * b.blocks <= kMaxTreeGroups;
 }
 
 aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
   const bool same = a.p.q_dtype == (int)c_dtype, full = c_dtype == AATC_F32;
-  const Blocks b = blocks_of(a.drafts, a.p.G, same && !full ? kMostSame : kMostOther);
+  const Blocks b = blocks_of(a.drafts, a.p.G);
   const int rows = a.p.batch * a.p.n_kv_heads;
   a.blocks = b.blocks;
   a.block_cols = b.cols();
   a.units = units_of(b.blocks);
-  a.quantum = b.cols() == kGroup ? kNarrowQuantum : kWideQuantum;
+  a.quantum = quantum_of(b.cols());
   a.p.parts = static_cast<Partial*>(workspace);
   const int64_t most = rows <= a.units ? a.units : (int64_t)rows + a.units;
   const int64_t grid = (most + 7) / 8 * 8 * b.blocks;
@@ -875,10 +939,7 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
     switch (10 * b.cw + b.c) {
       case 11: return launch(tree_narrow_kernel<M, QT>, 8);
       case 41: return launch(tree_wide_kernel<M, QT, 1, 4, W>, W);
-      case 42: return launch(tree_wide_kernel<M, QT, 2, 4, W>, W);
-      default:
-        if constexpr (W == 8) return launch(tree_wide_kernel<M, QT, 2, 8, W>, W);
-        else return AATC_E_UNSUPPORTED;            // (no such block)
+      default: return launch(tree_wide_kernel<M, QT, 2, 4, W>, W);
     }
   };
   using One = std::integral_constant<int, 1>;

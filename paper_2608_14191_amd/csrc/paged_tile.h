@@ -87,21 +87,25 @@ struct Half16 {
   static __device__ int key_block(int n) { return n >> 2; }
   static __device__ int value_block(int g) { return g; }
   // A tile in LDS: piece c (16 bytes) of a token's row lies in the place c ^ turn_of(row), so that
-  // the eight rows that a quarter of a wave reads a key operand from are in different banks.  Register
-  // u (of eight) of a lane's keys is at key_place(u & 1) + key_offset(u), of its values at
-  // value_place(value_turn(u)) + value_offset(u).
+  // the rows that a part of a wave reads at one time are in different banks.  Register u (of eight) of a
+  // lane's keys is at (key_place ^ 64 key_flip(u)) + key_offset(u).
   static constexpr int kRow = 256;
-  static __device__ int turn_of(int row) { return (row & 3) | (row >> 1 & 4); }
-  static __device__ int key_place(int odd, int n, int g) {
-    const int row = key_token(0, n), t = turn_of(row);
-    return row * kRow + 16 * (g ^ (t & 3)) + 64 * (odd ^ (t >> 2));
+  static __device__ int turn_of(int row) { return (row & 3) << 1 | (row & 8); }
+  static __device__ int key_place(int n, int g) {
+    const int row = key_token(0, n);
+    return row * kRow + 16 * (g ^ turn_of(row));
   }
-  static constexpr int key_offset(int u) { return u / 4 * 4 * kRow + u % 4 / 2 * 128; }
-  static __device__ int value_place(int turn, int n, int g) {
-    return 8 * g * kRow + 16 * (n ^ (turn_of(8 * g) | turn));
+  static constexpr int key_flip(int u) { return u % 4; }
+  static constexpr int key_offset(int u) { return u / 4 * 4 * kRow; }
+  // Values are read turned (ds_read_b64_tr_b16: of sixteen lanes, lane 4 e + q reads four channels of
+  // token e, lane i gets channel i of the four tokens): product j has channels 16 j + 0 .. 15, its
+  // tokens 8 g + 4 x + e at (value_place ^ 32 j) + 4 kRow x.
+  static constexpr bool kReadsTurned = true;
+  static __device__ int value_place(int n, int g) {
+    const int row = 8 * g + (n >> 2);
+    return row * kRow + 16 * ((n >> 1 & 1) ^ turn_of(row)) + 8 * (n & 1);
   }
-  static constexpr int value_turn(int u) { return u & 3; }
-  static constexpr int value_offset(int u) { return u * kRow; }
+  static __device__ int turned_channel(int j, int i, int g) { return 16 * j + 4 * g + i; }
 
   static __device__ v4f mfma(v8 a, v8 b, v4f c) {
     if constexpr (kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -208,6 +212,35 @@ struct Half16 {
         t.a[j][d] = __builtin_amdgcn_perm(v.r[2 * d + 1][j / 2], v.r[2 * d][j / 2],
                                           j & 1 ? 0x07060302u : 0x05040100u);
   }
+  // Token e of the lane's counts as zeros unless it is in `on` (bit e).
+  static __device__ void keep_turned(Turned& t, unsigned on) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t mask = (on >> (2 * d) & 1u ? 0xffffu : 0u) | (on >> (2 * d + 1) & 1u ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t.a[j][d] &= mask;
+    }
+  }
+  // Whether any of the lane's values may be not finite, and those as zeros.
+  static __device__ bool any_bad(const Turned& t) {
+    Values v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.r[j] = t.a[j];
+    return any_bad(v);
+  }
+  static __device__ bool bad16(uint32_t x) {
+    const uint32_t up = kF16 ? 0x7c00u : 0x7f80u;
+    return (x & up) == up;
+  }
+  static __device__ void drop_bad(Turned& t) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t x = t.a[j][d];
+        t.a[j][d] = (bad16(x) ? 0u : x & 0xffffu) | (bad16(x >> 16) ? 0u : x & 0xffff0000u);
+      }
+  }
   // P as terms of 8 tokens.  bf16: the upper half of the number, the upper half of the rest, the rest
   // (exact: 8 bits each of 24).  f16: towards zero, then the rest to the nearest (2^-22 of it).
   struct Weights {
@@ -304,19 +337,18 @@ struct Full32 {
   static __device__ int key_token(int, int n) { return n; }
   static __device__ int key_block(int n) { return n >> 3; }
   static __device__ int value_block(int g) { return g >> 1; }
-  // (as Half16's)
+  // (as Half16's; values are read as rows: register u at (value_place ^ 16 value_flip(u)) +
+  // value_offset(u))
   static constexpr int kRow = 512;
   static __device__ int turn_of(int row) { return row & 7; }
-  static __device__ int key_place(int odd, int n, int g) {
-    const int t = turn_of(n);
-    return n * kRow + 16 * (g ^ (t & 3)) + 64 * (odd ^ (t >> 2));
-  }
+  static __device__ int key_place(int n, int g) { return n * kRow + 16 * (g ^ turn_of(n)); }
+  static constexpr int key_flip(int u) { return u % 2; }
   static constexpr int key_offset(int u) { return u / 2 * 128; }
-  static __device__ int value_place(int turn, int n, int g) {
-    return 4 * g * kRow + 16 * (n ^ (turn_of(4 * g) | turn));
-  }
-  static constexpr int value_turn(int u) { return u / 2; }
+  static constexpr bool kReadsTurned = false;
+  static __device__ int value_place(int n, int g) { return 4 * g * kRow + 16 * (n ^ turn_of(4 * g)); }
+  static constexpr int value_flip(int u) { return u / 2; }
   static constexpr int value_offset(int u) { return u / 2 * kRow + u % 2 * 256; }
+  static __device__ int turned_channel(int j, int i, int g) { return channel(j, i, g); }
   static __device__ v4f mfma(float a, float b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
   }
