@@ -255,8 +255,9 @@ struct TreeWave {
       const int col = first + c * kGroup + n;
       const bool on = col < columns;
       const int x = block * a.block_cols + (on ? col : 0), i = x / p.G, j = x - i * p.G;
+      // (columns that are not there are the first one's: a choice would wait for the load)
       q[c].load(p.q, p.q_dtype,
-                ((int64_t)r.seq * a.drafts + i) * p.q_stride + (int64_t)(r.kvh * p.G + j) * kD, on, g);
+                ((int64_t)r.seq * a.drafts + i) * p.q_stride + (int64_t)(r.kvh * p.G + j) * kD, true, g);
       if (g == 0) {                                // (waves with the same columns write the same)
         space.draft[col] = i;
         space.slope[col] = p.slopes && on ? p.slopes[r.kvh * p.G + j] * kLog2e : 0.f;
@@ -648,6 +649,7 @@ __global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
   if (!find_run<TT, W>(a, (int)blockIdx.x, sh.scan, sh.found, r)) return;
   const int columns = r.m * p.G;
   const TreePages pages(p, r.seq, r.kvh);
+  TreeWave<M, QT, 1, false> x(a, r, sh.info, 0, 0, columns);
   typename M::Keys key;
   typename M::Values val;
   auto load_keys = [&](int t0, int page) {
@@ -665,7 +667,6 @@ __global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
     load_keys(t0, key_page(t0));
     load_values(t0, vp);
   }
-  TreeWave<M, QT, 1, false> x(a, r, sh.info, 0, 0, columns);
   if (wave == W - 1) find_families(a, r, sh.info);
   __syncthreads();
   for (int i = begin; i < last; i += W) {
@@ -690,8 +691,8 @@ __global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
 // More columns.  A stage has kStage tiles: 16 KiB of keys and 16 KiB of values, loaded straight into
 // LDS, kRing - 1 stages ahead of the one that is computed.  Wave w has 16 C columns from
 // (w / TW) 16 C on and every TW-th tile.
-constexpr int kStage = 2, kRing = 4;
-constexpr int kHalfStage = kStage * 8192;          // bytes of a stage's keys, and of its values
+constexpr int kRingTiles = 8;
+constexpr int kValueRing = kRingTiles * 8192;      // the values' place in the ring, behind all keys
 // Waits until no more than n vector loads are outstanding, and for LDS.
 template <int N>
 __device__ inline void wait_loads() {
@@ -735,11 +736,11 @@ __device__ inline void read_values(typename M::Values& to, uint32_t at) {
         "=&v"(x[7])
       : "v"(p[M::value_flip(0)]), "v"(p[M::value_flip(1)]), "v"(p[M::value_flip(2)]),
         "v"(p[M::value_flip(3)]), "v"(p[M::value_flip(4)]), "v"(p[M::value_flip(5)]),
-        "v"(p[M::value_flip(6)]), "v"(p[M::value_flip(7)]), "n"(kHalfStage + M::value_offset(0)),
-        "n"(kHalfStage + M::value_offset(1)), "n"(kHalfStage + M::value_offset(2)),
-        "n"(kHalfStage + M::value_offset(3)), "n"(kHalfStage + M::value_offset(4)),
-        "n"(kHalfStage + M::value_offset(5)), "n"(kHalfStage + M::value_offset(6)),
-        "n"(kHalfStage + M::value_offset(7))
+        "v"(p[M::value_flip(6)]), "v"(p[M::value_flip(7)]), "n"(M::value_offset(0)),
+        "n"(M::value_offset(1)), "n"(M::value_offset(2)),
+        "n"(M::value_offset(3)), "n"(M::value_offset(4)),
+        "n"(M::value_offset(5)), "n"(M::value_offset(6)),
+        "n"(M::value_offset(7))
       : "memory");
   __builtin_memcpy(&to, x, sizeof x);
 }
@@ -762,21 +763,22 @@ __device__ inline void read_turned(typename M::Turned& to, uint32_t at) {
         "=&v"(x[5][0]), "=&v"(x[5][1]), "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]),
         "=&v"(x[7][1])
       : "v"(at), "v"(at ^ 32u), "v"(at ^ 64u), "v"(at ^ 96u), "v"(at ^ 128u), "v"(at ^ 160u),
-        "v"(at ^ 192u), "v"(at ^ 224u), "n"(kHalfStage), "n"(kHalfStage + 4 * M::kRow)
+        "v"(at ^ 192u), "v"(at ^ 224u), "n"(0), "n"(4 * M::kRow)
       : "memory");
 #pragma unroll
   for (int j = 0; j < 8; ++j) to.a[j] = (v4u){x[j][0][0], x[j][0][1], x[j][1][0], x[j][1][1]};
 }
 
-template <class M, int QT, int C, int CW, int W>
+template <class M, int QT, int C, int CW, int W, int kStage>
 __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
   constexpr int TT = M::kTokens, NM = M::kMine, TW = W / CW;
   constexpr int kRow = M::kRow;
+  constexpr int kRing = kRingTiles / kStage;
   constexpr int PT = kStage * TT / W;              // tokens of a stage that a wave loads
   constexpr int kPer = 1024 / kRow;                // tokens of one load of the wave
   static_assert(TW >= 1 && TW <= kStage && 16 * C * CW <= kMostCols, "a tile for every wave");
   __shared__ TreeSpace<W> sh;
-  __shared__ __align__(1024) char ring[kRing * 2 * kHalfStage];
+  __shared__ __align__(1024) char ring[2 * kValueRing];
   __shared__ int there[kRing][kStage * TT / 8];    // whether the page of 8 tokens is
   const PagedArgs& p = a.p;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -790,6 +792,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
   const int columns = min(r.m * p.G - cb * a.block_cols, a.block_cols);
   if (columns <= 0) return;                        // (uniform)
   const TreePages pages(p, r.seq, r.kvh);
+  // (queries first: their wait would be one for all loads before them)
+  const int cw = wave / TW, tw = wave % TW;
+  TreeWave<M, QT, C, M::kReadsTurned> x(a, r, sh.info, cb, cw * C * kGroup, columns);
 
   // This wave's PT tokens of a stage: their first one, pages a stage ahead of the loads, and those.
   // (Pages by scalar loads: a vector load's wait would be one for all loads before it.  Every stage has
@@ -815,11 +820,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
       const int at = i * kPer + lane / (kRow / 16), c = lane % (kRow / 16);
       const int64_t from = pages.slot_of(t + at, page[i * kPer / 8]) +
                            16 * (c ^ M::turn_of((wave * PT + at) % TT));
-      char* to = ring + slot * (2 * kHalfStage) + (wave * PT + i * kPer) * kRow;
+      char* to = ring + slot * (kStage * 8192) + (wave * PT + i * kPer) * kRow;
       using Global = const __attribute__((address_space(1))) void*;
       using Local = __attribute__((address_space(3))) void*;
       __builtin_amdgcn_global_load_lds((Global)(p.k + from), (Local)to, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kHalfStage), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kValueRing), 16, 0, 0);
     }
     if (lane < PT / 8) {
       int on = 0;
@@ -835,8 +840,6 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
   for (int s = 0; s < kRing; ++s) fetch_pages(s, page[s]);
 #pragma unroll
   for (int s = 0; s < kRing - 1; ++s) issue(s, page[s]);
-  const int cw = wave / TW, tw = wave % TW;
-  TreeWave<M, QT, C, M::kReadsTurned> x(a, r, sh.info, cb, cw * C * kGroup, columns);
   if (wave == W - 1) find_families(a, r, sh.info);
   const bool busy = cw * C * kGroup < columns;     // (uniform)
   // Where the lane's pieces of a tile are (a ring aligned to more than a row: pieces differ in bits of
@@ -858,17 +861,17 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
         const int i = r.first + s * kStage + k;
         if (i >= r.last) break;                    // (uniform)
         typename M::Keys key;
-        const uint32_t from = base + slot * (2 * kHalfStage) + k * (TT * kRow);
+        const uint32_t from = base + slot * (kStage * 8192) + k * (TT * kRow);
         read_keys<M>(key, from + key0);
         const int t0 = r.rt.token(i, TT);
         const bool on = there[slot][k * TT / 8 + M::value_block(g)] != 0;
         if constexpr (M::kReadsTurned) {
           typename M::Turned turned;
-          read_turned<M>(turned, from + value0);
+          read_turned<M>(turned, from + kValueRing + value0);
           x.step(t0, on, key, turned);
         } else {
           typename M::Values val;
-          read_values<M>(val, from + value0);
+          read_values<M>(val, from + kValueRing + value0);
           x.step(t0, on, key, val, [] {}, [] {});
         }
       }
@@ -893,7 +896,7 @@ Blocks blocks_of(int drafts, int G) {
   const int groups = (drafts * G + kGroup - 1) / kGroup;
   if (groups == 1) return {1, 1, 1};
   const int blocks = (groups + 7) / 8, each = (groups + blocks - 1) / blocks;
-  return {blocks, each <= 4 ? 1 : 2, 4};
+  return {blocks, each <= 2 ? 1 : 2, each <= 4 ? 2 : 4};
 }
 int units_of(int blocks) { return std::max(1, kTreeGroups / blocks); }
 
@@ -938,8 +941,9 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
     constexpr int W = QT == 1 && sizeof(typename M::Elem) == 2 ? 8 : 4;
     switch (10 * b.cw + b.c) {
       case 11: return launch(tree_narrow_kernel<M, QT>, 8);
-      case 41: return launch(tree_wide_kernel<M, QT, 1, 4, W>, W);
-      default: return launch(tree_wide_kernel<M, QT, 2, 4, W>, W);
+      case 21: return launch(tree_wide_kernel<M, QT, 1, 2, W, W == 8 ? 4 : 2>, W);
+      case 22: return launch(tree_wide_kernel<M, QT, 2, 2, W, W == 8 ? 4 : 2>, W);
+      default: return launch(tree_wide_kernel<M, QT, 2, 4, W, 2>, W);
     }
   };
   using One = std::integral_constant<int, 1>;
