@@ -22,6 +22,7 @@
 #include "paged_plan.h"
 #include "paged_tile.h"
 #include "params.h"
+#include "wave_scan.h"
 
 namespace aatc {
 namespace {
@@ -56,16 +57,13 @@ struct TreeInfo {
   float slope[kMostCols];
 };
 
+constexpr int kLaneRows = 256;                    // sequences that lanes of a wave have to themselves
+
 // This thread's number plus those of the threads before it; `total`: of all.
 template <int W>
 __device__ inline int scan_all(int x, int* space, int& total) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int incl = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(incl, o, 64);
-    incl += lane >= o ? up : 0;
-  }
+  int incl = wave_scan_sum(x);
   __syncthreads();                                 // (the space's last readers are done)
   if (lane == 63) space[wave] = incl;
   __syncthreads();
@@ -108,13 +106,59 @@ __device__ inline bool find_run(const TreeArgs& a, int unit, int (*scan)[W], int
     const int m = drafts_of(a, b);
     return row_tiles(cached_of(a, b) + m, window_of(p.window, m), p.sink, TT);
   };
+  // Rows that fit the chip are cut into runs that do; more rows into runs as long as the average
+  // share: no more than `units` of them beyond one a row.
+  auto share = [&](int tiles, int longest, int rows, auto count) {
+    return rows * heads <= a.units
+               ? a.quantum * smallest_rounds(tiles * heads, longest, rows * heads, a.units, a.quantum, count)
+               : max((int)(((int64_t)tiles * heads + a.units - 1) / a.units), kRoundsMin * a.quantum);
+  };
   int before = 0, shared = 0, most;
   r.seq = 0;
   if (p.batch == 1) {
     if (drafts_of(a, 0) == 0) return false;
     r.rt = tiles_of(0);
-    most = a.quantum * smallest_rounds(r.rt.n * heads, r.rt.n, heads, a.units, a.quantum,
-                                       [&](int q) { return heads * runs_of(r.rt.n, q); });
+    most = share(r.rt.n, r.rt.n, 1, [&](int q) { return heads * runs_of(r.rt.n, q); });
+  } else if (p.batch <= kLaneRows) {
+    // Some sequences a lane; every wave does the same.
+    constexpr int S = kLaneRows / 64;
+    int n_of[S], tiles = 0, rows = 0, longest = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int b = lane + 64 * i;
+      n_of[i] = b < p.batch && drafts_of(a, b) ? tiles_of(b).n : 0;
+      tiles += n_of[i];
+      rows += n_of[i] > 0;
+      longest = max(longest, n_of[i]);
+    }
+    tiles = wave_total(tiles);
+    if (tiles == 0) return false;
+    rows = wave_total(rows);
+    longest = __builtin_amdgcn_readlane(wave_scan(longest, 0, [](int x, int y) { return max(x, y); }), 63);
+    most = share(tiles, longest, rows, [&](int q) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < S; ++i) n += runs_of(n_of[i], q);
+      return heads * wave_total(n);
+    });
+    int runs = 0, in_shared = 0, owner = -1;       // of the sequences before
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int k = runs_of(n_of[i], most), mine = heads * k;
+      const int incl = runs + wave_scan_sum(mine);
+      const int at_shared = in_shared + wave_scan_sum(k > 1 ? mine : 0);
+      const uint64_t has = __builtin_amdgcn_ballot_w64(unit >= incl - mine && unit < incl);
+      if (has) {                                   // (one lane, of one of the rounds)
+        owner = __builtin_ctzll(has);
+        r.seq = owner + 64 * i;
+        before = __builtin_amdgcn_readlane(incl - mine, owner);
+        shared = __builtin_amdgcn_readlane(at_shared - (k > 1 ? mine : 0), owner);
+      }
+      runs = __builtin_amdgcn_readlane(incl, 63);
+      in_shared = __builtin_amdgcn_readlane(at_shared, 63);
+    }
+    if (owner < 0) return false;
+    r.rt = tiles_of(r.seq);
   } else {
     const int each = (p.batch + NT - 1) / NT;
     const int b0 = min(tid * each, p.batch), b1 = min(b0 + each, p.batch);
@@ -142,12 +186,7 @@ __device__ inline bool find_run(const TreeArgs& a, int unit, int (*scan)[W], int
       scan_all<W>(n, scan[0], all);
       return heads * all;
     };
-    // Rows that fit the chip are cut into runs that do; more rows into runs as long as the average
-    // share: no more than `units` of them beyond one a row.
-    if (rows * heads <= a.units)
-      most = a.quantum * smallest_rounds(tiles * heads, longest, rows * heads, a.units, a.quantum, runs);
-    else
-      most = max((int)(((int64_t)tiles * heads + a.units - 1) / a.units), kRoundsMin * a.quantum);
+    most = share(tiles, longest, rows, runs);
     // Which sequence has this run, and the runs and the shared rows' runs before it.
     int n = 0, s = 0, total, spare;
     for (int b = b0; b < b1; ++b) {
@@ -226,14 +265,24 @@ struct TreePages {
 };
 
 // What a wave has of C groups of columns, from column col0 of the workgroup's block on: running
-// maxima (exponents of 2), sums and value sums (acc[c][j][i]: channel channel(j, i, g) of column
-// 16 c + n).
+// maxima (exponents of 2), sums and value sums (acc[c][j][i]: channel M::channel(j, i, g), or where
+// values come turned M::turned_channel(j, i, g), of column 16 c + n).
 // TURNED: values come turned from LDS (product j then has other channels).
 template <class M, int QT, int C, bool TURNED>
 struct TreeWave {
   using Tile = M;
-  static __device__ int channel(int j, int i, int g) {
-    return TURNED ? M::turned_channel(j, i, g) : M::channel(j, i, g);
+  // A column's value sums, four channels at a time.
+  __device__ void store(int c, float* to) const {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if constexpr (TURNED) {
+        *reinterpret_cast<v4f*>(to + M::turned_channel(x, 0, g)) = acc[c][x];
+      } else {                                     // (channels of four products follow each other)
+        const int j = x / 4 * 4, i = x % 4;
+        *reinterpret_cast<v4f*>(to + M::channel(j, i, g)) =
+            (v4f){acc[c][j][i], acc[c][j + 1][i], acc[c][j + 2][i], acc[c][j + 3][i]};
+      }
+    }
   }
   static constexpr int TT = M::kTokens, NM = M::kMine;
   const PagedArgs& p;
@@ -305,23 +354,30 @@ struct TreeWave {
     if (p.slopes || !whole) {
       const int col = col0 + c * kGroup + n;
       const int draft = info.draft[col], pos = len + info.depth[draft];
-      const uint64_t family = info.family[draft];
-      const float slope = info.slope[col];
-      if (!whole) bits = 0u;
+      const int first = t0 + NM * g;
+      // Positions of the lane's tokens, where they matter.
+      auto at = [&](int e) {
+        const int j = min(max(first + e - len, 0), kMaxDrafts - 1);
+        return first + e < len ? first + e : len + info.depth[j];
+      };
+      if (p.slopes) {
+        const float slope = info.slope[col];
 #pragma unroll
-      for (int e = 0; e < NM; ++e) {
-        const int t = t0 + NM * g + e;
-        const int j = min(max(t - len, 0), kMaxDrafts - 1);
-        const int at = whole || t < len ? t : len + info.depth[j];
-        if (p.slopes) z[e] -= slope * (float)(pos - at);
-        if (!whole) {
-          // (no short circuits: selects, not branches)
-          const bool kin = (t < len) | ((t < end) & (bool)(family >> j & 1));
-          const bool near = (p.window == 0) | (pos - at < p.window) | (t < p.sink);
-          const bool on = there & kin & near;
-          z[e] = on ? z[e] : -INFINITY;
-          bits |= on ? 1u << e : 0u;
-        }
+        for (int e = 0; e < NM; ++e) z[e] -= slope * (float)(pos - (whole ? first + e : at(e)));
+      }
+      if (!whole) {
+        // Bit e: a token of the sequence, or a draft of the column's family (bits of no draft are 0).
+        const uint64_t family = info.family[draft];
+        const int j = first - len;
+        bits = (unsigned)(j >= 0 ? j < kMaxDrafts ? family >> j : 0
+                          : j <= -NM ? ~(uint64_t)0 : family << -j | (((uint64_t)1 << -j) - 1));
+        if (p.window)
+#pragma unroll
+          for (int e = 0; e < NM; ++e)
+            if (!((pos - at(e) < p.window) | (first + e < p.sink))) bits &= ~(1u << e);
+        bits = there ? bits & ((1u << NM) - 1u) : 0u;
+#pragma unroll
+        for (int e = 0; e < NM; ++e) z[e] = bits >> e & 1u ? z[e] : -INFINITY;
       }
     }
     return bits;
@@ -527,11 +583,7 @@ __device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, 
       sh.m[wave][n] = low ? kLowest : x.m_run[c];
       sh.l[wave][n] = low ? 1.f : l;
     }
-    float* mine = sums(wave) + n * (kD + 4);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mine[Wave::channel(j, i, g)] = x.acc[c][j][i];
+    x.store(c, sums(wave) + n * (kD + 4));
     __syncthreads();
     for (int y = tid; y < CW * kGroup * (kD / 4); y += NT) {
       const int h = y / (kD / 4) % kGroup, c4 = y % (kD / 4), w0 = y / (kGroup * (kD / 4)) * TW;

@@ -16,27 +16,12 @@
 #include "paged_tile.h"
 #include "params.h"
 #include "sparse.h"
+#include "wave_scan.h"
 
 namespace aatc {
 namespace {
 
 constexpr int kLowestStep = -50, kHighestStep = 100;
-
-// Over a wave, by shifts within rows of 16 lanes and broadcasts of rows' last lanes: lane l gets f of the
-// lanes up to l (the last one f of all).  `none`: what f leaves as it is.
-template <class F>
-__device__ inline int wave_scan(int x, int none, F f) {
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));      // row_shr:1
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));      // row_bcast:15
-  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));      // row_bcast:31
-  return x;
-}
-__device__ inline int wave_scan_sum(int x) {
-  return wave_scan(x, 0, [](int a, int b) { return a + b; });
-}
 
 // The exponent of the smallest power of two, from 2^-50 on, of which 127 reach `top` (finite, >= 0).
 __device__ inline int step_of(float top) {

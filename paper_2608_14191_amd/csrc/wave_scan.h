@@ -1,0 +1,27 @@
+// Scans over the lanes of a wave.  Device code; all lanes active.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+namespace aatc {
+namespace {
+
+// Over a wave, by shifts within rows of 16 lanes and broadcasts of rows' last lanes: lane l gets f of the
+// lanes up to l (the last one f of all).  `none`: what f leaves as it is.
+template <class F>
+__device__ inline int wave_scan(int x, int none, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));      // row_shr:1
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));      // row_bcast:15
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));      // row_bcast:31
+  return x;
+}
+__device__ inline int wave_scan_sum(int x) {
+  return wave_scan(x, 0, [](int a, int b) { return a + b; });
+}
+__device__ inline int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan_sum(x), 63); }
+
+}  // namespace
+}  // namespace aatc
