@@ -21,6 +21,7 @@ struct TreeArgs {
   int blocks, block_cols;         // a (sequence, KV head)'s queries: blocks of so many columns
   int units;                      // runs of tokens that fill the chip (each `blocks` workgroups)
   int quantum;                    // tiles
+  bool far;                       // pools that do not fit the caches: loads past them
 };
 
 size_t tree_workspace_bytes(int batch, int drafts, int n_q_heads, int n_kv_heads);

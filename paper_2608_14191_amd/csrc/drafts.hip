@@ -29,10 +29,10 @@ namespace {
 
 // One workgroup a compute unit, so that a row has few parts to join.
 constexpr int kTreeGroups = 256;
+// Or four, of the narrow kernel for more rows than these.
+constexpr int kFewRows = 128, kSmallGroups = 1024;
 constexpr int kGroup = 16;                        // columns of a group
 constexpr int kMostCols = 128;                    // of a workgroup
-// The workspace: part slots.  At most twice as many runs as fill the chip belong to shared rows.
-constexpr int kTreeSlots = 2 * kTreeGroups;
 // Runs are a multiple of so many tiles, twice that at least: what a workgroup computes in about the time
 // that the join takes.
 constexpr int quantum_of(int cols) { return cols <= 64 ? 8 : 4; }
@@ -621,7 +621,7 @@ constexpr int kJoinWaves = 8;
 template <int TT>
 __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) {
   constexpr int W = kJoinWaves, NT = 64 * W;
-  constexpr int kPairs = kMostCols + kTreeGroups;  // columns / parts of them, for each part
+  constexpr int kPairs = kMostCols + kSmallGroups;  // columns / parts of them, for each part
   __shared__ int scan[2][W], found[4];
   __shared__ float weight[kPairs], sum[kPairs], top[kMostCols], total[kMostCols];
   const PagedArgs& p = a.p;
@@ -687,11 +687,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) 
   }
 }
 
-// Up to 16 columns: eight waves, each with tiles of its own; keys and values one tile ahead, pages
-// two.
-template <class M, int QT>
-__global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
-  constexpr int W = 8, TT = M::kTokens, NM = M::kMine;
+// Up to 16 columns: every wave has tiles of its own; keys and values one tile ahead, pages two.  Few rows:
+// eight waves a workgroup, so that a row has few parts to join.  Many: four, whose runs are dealt more
+// evenly (384 rows of 129 float32 tiles: NNN us, eight 165).
+template <class M, int QT, int W>
+__global__ __launch_bounds__(64 * W, 2) void tree_narrow_kernel(TreeArgs a) {
+  constexpr int TT = M::kTokens, NM = M::kMine;
   __shared__ TreeSpace<W> sh;
   __shared__ __align__(16) float space[W * kSumsFloats];
   const PagedArgs& p = a.p;
@@ -744,6 +745,7 @@ __global__ __launch_bounds__(512, 2) void tree_narrow_kernel(TreeArgs a) {
 // LDS, kRing - 1 stages ahead of the one that is computed.  Wave w has 16 C columns from
 // (w / TW) 16 C on and every TW-th tile.
 constexpr int kRingTiles = 8;
+constexpr int kStreamed = 2;                       // cache policy nt
 constexpr int kValueRing = kRingTiles * 8192;      // the values' place in the ring, behind all keys
 // Waits until no more than n vector loads are outstanding, and for LDS.
 template <int N>
@@ -875,8 +877,13 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
       char* to = ring + slot * (kStage * 8192) + (wave * PT + i * kPer) * kRow;
       using Global = const __attribute__((address_space(1))) void*;
       using Local = __attribute__((address_space(3))) void*;
-      __builtin_amdgcn_global_load_lds((Global)(p.k + from), (Local)to, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kValueRing), 16, 0, 0);
+      if (a.far) {                                 // (uniform)
+        __builtin_amdgcn_global_load_lds((Global)(p.k + from), (Local)to, 16, 0, kStreamed);
+        __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kValueRing), 16, 0, kStreamed);
+      } else {
+        __builtin_amdgcn_global_load_lds((Global)(p.k + from), (Local)to, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((Global)(p.v + from), (Local)(to + kValueRing), 16, 0, 0);
+      }
     }
     if (lane < PT / 8) {
       int on = 0;
@@ -950,11 +957,15 @@ Blocks blocks_of(int drafts, int G) {
   const int blocks = (groups + 7) / 8, each = (groups + blocks - 1) / blocks;
   return {blocks, each <= 2 ? 1 : 2, each <= 4 ? 2 : 4};
 }
-int units_of(int blocks) { return std::max(1, kTreeGroups / blocks); }
+bool small_groups(const Blocks& b, int64_t rows) { return b.cols() == kGroup && rows > kFewRows; }
+int units_of(const Blocks& b, int64_t rows) {
+  return small_groups(b, rows) ? kSmallGroups : std::max(1, kTreeGroups / b.blocks);
+}
 
+// Part slots: runs that fit the chip, or at most twice as many where more rows than those are cut.
 size_t tree_parts_bytes(const Blocks& b, int64_t rows) {
-  const int slots = rows <= units_of(b.blocks) ? kTreeGroups : kTreeSlots;
-  return (size_t)slots * b.cols() * sizeof(Partial);
+  const int units = units_of(b, rows);
+  return (size_t)(rows <= units ? 1 : 2) * units * b.blocks * b.cols() * sizeof(Partial);
 }
 
 }  // namespace
@@ -967,7 +978,7 @@ bool tree_fits(int64_t batch, int drafts, int n_q_heads, int n_kv_heads) {
   const int64_t columns = (int64_t)drafts * (n_q_heads / n_kv_heads);
   if (columns > kMaxColumns) return false;
   const Blocks b = blocks_of(drafts, n_q_heads / n_kv_heads);
-  return (batch * n_kv_heads + kTreeGroups + 8) * b.blocks <= kMaxTreeGroups;
+  return (batch * n_kv_heads + kSmallGroups + 8) * b.blocks <= kMaxTreeGroups;
 }
 
 aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* stream) {
@@ -976,7 +987,7 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
   const int rows = a.p.batch * a.p.n_kv_heads;
   a.blocks = b.blocks;
   a.block_cols = b.cols();
-  a.units = units_of(b.blocks);
+  a.units = units_of(b, rows);
   a.quantum = quantum_of(b.cols());
   a.p.parts = static_cast<Partial*>(workspace);
   const int64_t most = rows <= a.units ? a.units : (int64_t)rows + a.units;
@@ -986,26 +997,37 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * waves), 0, st, a);
     return hipGetLastError() == hipSuccess ? AATC_OK : AATC_E_DEVICE;
   };
-  auto launch_as = [&](auto m, auto qt) {
+  using One = std::integral_constant<int, 1>;
+  using Three = std::integral_constant<int, 3>;
+  auto launch_narrow = [&](auto near, auto past, auto qt) {
+    constexpr int QT = decltype(qt)::value;
+    if (small_groups(b, rows))
+      return a.far ? launch(tree_narrow_kernel<decltype(past), QT, 4>, 4)
+                   : launch(tree_narrow_kernel<decltype(near), QT, 4>, 4);
+    return a.far ? launch(tree_narrow_kernel<decltype(past), QT, 8>, 8)
+                 : launch(tree_narrow_kernel<decltype(near), QT, 8>, 8);
+  };
+  auto launch_wide = [&](auto m, auto qt) {
     using M = decltype(m);
     constexpr int QT = decltype(qt)::value;
     // Queries of one 16-bit term leave room for two waves a SIMD.
-    constexpr int W = QT == 1 && sizeof(typename M::Elem) == 2 ? 8 : 4;
-    switch (10 * b.cw + b.c) {
-      case 11: return launch(tree_narrow_kernel<M, QT>, 8);
-      case 21: return launch(tree_wide_kernel<M, QT, 1, 2, W, W == 8 ? 4 : 2>, W);
-      case 22: return launch(tree_wide_kernel<M, QT, 2, 2, W, W == 8 ? 4 : 2>, W);
-      default: return launch(tree_wide_kernel<M, QT, 2, 4, W, 2>, W);
-    }
+    constexpr int W = QT == 1 && sizeof(typename M::Elem) == 2 ? 8 : 4, S = W == 8 ? 4 : 2;
+    if (b.cw == 2)
+      return b.c == 1 ? launch(tree_wide_kernel<M, QT, 1, 2, W, S>, W)
+                      : launch(tree_wide_kernel<M, QT, 2, 2, W, S>, W);
+    return launch(tree_wide_kernel<M, QT, 2, 4, W, 2>, W);
   };
-  using One = std::integral_constant<int, 1>;
-  using Three = std::integral_constant<int, 3>;
+  auto launch_as = [&](auto near, auto past, auto qt) {
+    return b.cols() == kGroup ? launch_narrow(near, past, qt) : launch_wide(near, qt);
+  };
+  auto launch_type = [&](auto near, auto past) {
+    return same ? launch_as(near, past, One{}) : launch_as(near, past, Three{});
+  };
+  a.far = pools_far(a.p, c_dtype);
   const aatc_status e =
-      full ? launch_as(Full32<false>{}, One{})
-      : c_dtype == AATC_BF16 ? same ? launch_as(Half16<__bf16, false>{}, One{})
-                                    : launch_as(Half16<__bf16, false>{}, Three{})
-      : same ? launch_as(Half16<_Float16, false>{}, One{})
-             : launch_as(Half16<_Float16, false>{}, Three{});
+      full ? launch_as(Full32<false>{}, Full32<true>{}, One{})
+      : c_dtype == AATC_BF16 ? launch_type(Half16<__bf16, false>{}, Half16<__bf16, true>{})
+                             : launch_type(Half16<_Float16, false>{}, Half16<_Float16, true>{});
   // (a table that holds no more than a shortest run's tokens has no shared rows)
   const int tt = full ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   if (e != AATC_OK || (a.p.len_max + a.drafts) / tt < kRoundsMin * a.quantum) return e;

@@ -639,10 +639,7 @@ aatc_status launch_paged(PagedArgs a, aatc_dtype c_dtype, void* workspace, void*
                     : launch_as(Half16<_Float16, F>{}, Three{});
     }
   };
-  const int64_t page_bytes = ((int64_t)1 << a.page_shift) * a.n_kv_heads * kD *
-                             (c_dtype == AATC_F32 ? 4 : 2);
-  const bool far = 2 * page_bytes > kFarBytes / a.n_pages;       // (both pools)
-  return far ? launch_type(std::true_type{}) : launch_type(std::false_type{});
+  return pools_far(a, c_dtype) ? launch_type(std::true_type{}) : launch_type(std::false_type{});
 }
 
 }  // namespace aatc

@@ -9,6 +9,7 @@
 #include <cfloat>
 
 #include "aatc.h"
+#include "paged.h"
 #include "params.h"
 
 namespace aatc {
@@ -65,6 +66,11 @@ __device__ inline void load_queries(const void* q, int dtype, int64_t i, bool on
 // and 30.7), smaller ones may be found there again (1 x 4000 tokens 14.7 and 13.0).  The pool is what
 // counts, whatever part of it the sequences have.
 constexpr int64_t kFarBytes = (int64_t)128 << 20;
+inline bool pools_far(const PagedArgs& a, aatc_dtype c_dtype) {
+  const int64_t page_bytes = ((int64_t)1 << a.page_shift) * a.n_kv_heads * kD *
+                             (c_dtype == AATC_F32 ? 4 : 2);
+  return 2 * page_bytes > kFarBytes / a.n_pages;                 // (both pools)
+}
 template <bool FAR, class V>
 __device__ inline V load16(const char* p) {
   if constexpr (FAR) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
