@@ -191,15 +191,8 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
       float most = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) most = fmaxf(most, fmaxf(fabsf(x.largest(i)), fabsf(x.smallest(i))));
-      // (over the lanes of a token: rotations within rows of 16, and a swap of two rows)
-      auto over = [&](auto ctrl) {
-        most = fmaxf(most, __uint_as_float(__builtin_amdgcn_update_dpp(
-                               0, (int)__float_as_uint(most), decltype(ctrl)::value, 0xf, 0xf, true)));
-      };
-      over(std::integral_constant<int, 0x128>{});
-      over(std::integral_constant<int, 0x124>{});
-      over(std::integral_constant<int, 0x122>{});
-      over(std::integral_constant<int, 0x121>{});
+      // (over the lanes of a token: rows of 16, and a swap of two rows)
+      most = row_max(most);
       if constexpr (L == 32) {
         auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(most), __float_as_uint(most), false, false);
         most = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -361,9 +354,7 @@ __global__ __launch_bounds__(256) void score_kernel(SparseArgs a) {
       for (int i = 0; i < 4; ++i) best[i] = e == kNoSay ? best[i] : fmaxf(best[i], (float)sum[i] * w);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) best[i] = fmaxf(best[i], __shfl_xor(best[i], o, 64));
+    for (int i = 0; i < 4; ++i) best[i] = row_max(best[i]);
     // Lane (n, g), n < 4, has page 4 g + n of the tile.
     const float mine = n == 0 ? best[0] : n == 1 ? best[1] : n == 2 ? best[2] : best[3];
     const int from = (lane & 48) | ((4 * g + n) & 15);
@@ -812,11 +803,10 @@ aatc_status launch_sparse(SparseArgs a, aatc_dtype c_dtype, void* workspace, voi
     // Few pages in small chunks, for the chip's sake; many in large ones, whose queries' codes count less.
     const int64_t pairs = (int64_t)p.batch * p.n_kv_heads;
     const bool many = pairs * p.max_pages >= 256 * 1024;
-    const int chunk = many ? 256 : 64;
+    const int chunk = many || p.hg > 1 ? 256 : 64;
     const dim3 groups((unsigned)(pairs * ((p.max_pages + chunk - 1) / chunk)));
     if (p.hg > 1)
-      hipLaunchKernelGGL((score_kernel<false, 4>), dim3((unsigned)(pairs * ((p.max_pages + 255) / 256))),
-                         dim3(256), 0, st, a);
+      hipLaunchKernelGGL((score_kernel<false, 4>), groups, dim3(256), 0, st, a);
     else if (many)
       hipLaunchKernelGGL((score_kernel<true, 4>), groups, dim3(256), 0, st, a);
     else

@@ -23,5 +23,15 @@ __device__ inline int wave_scan_sum(int x) {
 }
 __device__ inline int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan_sum(x), 63); }
 
+// Over each row of 16 lanes, by rotations: every lane gets the row's largest.
+template <int CTRL>
+__device__ inline float row_max_step(float x) {
+  return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf,
+                                                                         0xf, true)));
+}
+__device__ inline float row_max(float x) {
+  return row_max_step<0x121>(row_max_step<0x122>(row_max_step<0x124>(row_max_step<0x128>(x))));
+}
+
 }  // namespace
 }  // namespace aatc
