@@ -78,8 +78,8 @@ aatc_status aatc_paged_tree_attention(const aatc_paged_cache* cache, const aatc_
  * path         device [batch][max_draft] int32: the accepted drafts, ascending, -1 behind them.
  * accepted     device [batch] int32: how many (0 without drafts).
  * next         device [batch] int32: chosen after the last of them (-1 without drafts).
- * len_out      device [batch] int32: seq_len, clamped as below, + accepted; another buffer than
- *              seq_len.
+ * len_out      device [batch] int32: seq_len, clamped as below, + accepted.
+ * No output overlaps an input or another output: AATC_E_INVALID.
  * seq_len, n_draft, parent, max_draft: as in aatc_paged_tree_attention (seq_len clamped likewise).
  * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; max_draft), AATC_E_DEVICE.
  */

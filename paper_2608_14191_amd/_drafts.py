@@ -53,14 +53,26 @@ def _trees(func: str, seq_len, n_draft, parent, batch: int, max_draft: int):
         _list(func, "parent", parent, batch * max_draft)
 
 
+def _draft_stride(func: str, q, batch: int, max_draft: int) -> int:
+    """Elements between drafts of a view [batch * max_draft][heads][128] or [batch][max_draft][...]."""
+    if q.dim() < 4 or max_draft == 1:
+        if q.shape[0] < batch * max_draft:
+            _refuse(func, f"q has {q.shape[0]} tokens of {batch * max_draft}")
+        return q.stride(0)
+    if q.shape[0] < batch or q.shape[1] != max_draft or \
+            (batch > 1 and q.stride(0) != max_draft * q.stride(1)):
+        _refuse(func, f"q's {batch} x {max_draft} drafts do not lie at equal steps")
+    return q.stride(1)
+
+
 def aatc_paged_tree_attention(cache: PagedCache, table, seq_len, batch: int, max_draft: int,
                               n_q_heads: int, q, softmax_scale: float, out, workspace,
                               q_tok_stride: int = None, n_draft=None, parent=None, window: int = 0,
                               sink: int = 0, softcap: float = 0.0, slopes=None, lse=None,
                               stream=None):
     """Attention of max_draft drafted tokens per sequence (q: batch * max_draft tokens of
-    [n_q_heads][128], q_tok_stride elements apart, by default as the tensor's first dimension has
-    them) over the pages; parent int32 [batch][max_draft] or None (a chain); out
+    [n_q_heads][128], q_tok_stride elements apart, by default as the tensor's strides have them)
+    over the pages; parent int32 [batch][max_draft] or None (a chain); out
     [batch][max_draft][n_q_heads][128] and lse [batch][max_draft][n_q_heads] in float32."""
     f = "aatc_paged_tree_attention"
     device = _on_device(f, seq_len, n_draft, parent, q, out, workspace, slopes, lse,
@@ -74,9 +86,7 @@ def aatc_paged_tree_attention(cache: PagedCache, table, seq_len, batch: int, max
         _floats(f, "slopes", slopes, n_q_heads)
     stride = n_q_heads * HEAD_DIM if q_tok_stride is None else q_tok_stride
     if q_tok_stride is None and n > 1 and not q.is_contiguous():
-        if q.shape[0] < n:
-            _refuse(f, f"q has {q.shape[0]} tokens of {n}")
-        stride = q.stride(0)
+        stride = _draft_stride(f, q, batch, max_draft)
     _tokens(f, "q", q, n, stride, n_q_heads)
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), _ptr(n_draft), _ptr(parent), batch,

@@ -16,6 +16,15 @@ aatc_status check_trees(const int32_t* seq_len, const int32_t* n_draft, const in
   return max_draft <= kMaxDrafts ? AATC_OK : AATC_E_UNSUPPORTED;
 }
 
+struct List {
+  const int32_t* at;
+  int64_t n;
+};
+bool overlap(const List& x, const List& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+  return a && b && a < b + (uintptr_t)y.n * 4 && b < a + (uintptr_t)x.n * 4;
+}
+
 }  // namespace
 
 extern "C" size_t aatc_paged_tree_workspace_bytes(int32_t batch, int32_t max_draft,
@@ -84,16 +93,18 @@ extern "C" aatc_status aatc_paged_tree_accept(
     if (n_layers > 1 && (layer_stride < kD || layer_stride % (16 / size) ||
                          layer_stride >= ((int64_t)1 << 40)))
       return AATC_E_INVALID;
-    // (every workgroup of a sequence reads the inputs: none of them is an output too)
-    const void* in[] = {drafted, chosen, seq_len, n_draft, parent, table->table};
-    const void* res[] = {path, accepted, next, len_out};
-    for (const void* x : {in[0], in[1], res[0], res[1], res[2], res[3]})
-      if (!x || !aligned(x, 4)) return AATC_E_INVALID;
+    // (every workgroup of a sequence reads the inputs: no output overlaps one, or another)
+    const int64_t each = (int64_t)batch * max_draft;
+    const List in[] = {{drafted, each}, {chosen, each}, {seq_len, batch}, {n_draft, batch},
+                       {parent, each}, {table->table, (batch - 1) * table->stride + table->max_pages}};
+    const List res[] = {{path, each}, {accepted, batch}, {next, batch}, {len_out, batch}};
+    for (const List& x : {in[0], in[1], res[0], res[1], res[2], res[3]})
+      if (!x.at || !aligned(x.at, 4)) return AATC_E_INVALID;
     for (int i = 0; i < 4; ++i) {
-      for (const void* x : in)
-        if (res[i] == x) return AATC_E_INVALID;
+      for (const List& x : in)
+        if (overlap(res[i], x)) return AATC_E_INVALID;
       for (int j = 0; j < i; ++j)
-        if (res[i] == res[j]) return AATC_E_INVALID;
+        if (overlap(res[i], res[j])) return AATC_E_INVALID;
     }
     AcceptArgs a{};
     a.k = static_cast<char*>(cache->k_pages);
