@@ -689,7 +689,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) 
 
 // Up to 16 columns: every wave has tiles of its own; keys and values one tile ahead, pages two.  Few rows:
 // eight waves a workgroup, so that a row has few parts to join.  Many: four, whose runs are dealt more
-// evenly (384 rows of 129 float32 tiles: NNN us, eight 165).
+// evenly (384 rows of 129 float32 tiles: 157 us, eight 165).
 template <class M, int QT, int W>
 __global__ __launch_bounds__(64 * W, 2) void tree_narrow_kernel(TreeArgs a) {
   constexpr int TT = M::kTokens, NM = M::kMine;
