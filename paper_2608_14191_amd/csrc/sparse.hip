@@ -233,8 +233,8 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
 // Keys in the order of the scores: 0 for a page that is not there, kAlways for one picked always.
 constexpr uint32_t kAlways = 0xffffffffu;
 __device__ inline uint32_t key_of(float score) {
-  const uint32_t bits = __float_as_uint(score);
-  return bits ^ ((int32_t)bits < 0 ? 0xffffffffu : 0x80000000u);
+  const uint32_t bits = __float_as_uint(score), key = bits ^ ((int32_t)bits < 0 ? 0xffffffffu : 0x80000000u);
+  return min(max(key, 1u), kAlways - 1u);          // (scales that were never set may be any NaN)
 }
 
 // Queries of up to 16 heads in 8 bits, as the matrix operand of lane (n, g): head n's channels 16 g ..

@@ -233,6 +233,21 @@ def test_keys_and_queries_that_are_not_finite():
     assert torch.isfinite(got[1, :2]).all() and torch.equal(clean["q"].isnan(), c["q"].isnan())
 
 
+def test_scales_that_were_never_set():
+    """Any bits in some pages' bounds: as many pages as there is room for, in order, and no more."""
+    for bits in (0x7fffffff, -1, 0x7fc00000, -4194304, 0x7f800001):
+        c = _case(25, [320, 250], 4, 2, 16)
+        wild = torch.full(c["scales"].shape, bits, dtype=torch.int32).view(torch.float32)
+        c["scales"][::2] = wild[::2]
+        c["codes"][::3] = -128
+        picked, got, lse = _run(c, 6)
+        for b, pages in ((0, 20), (1, 16)):
+            for h in range(2):
+                x = picked[b, h].tolist()
+                assert x == sorted(set(x)) and x[0] == 0 and x[-1] == pages - 1
+        assert torch.isfinite(got).all() and torch.isfinite(lse).all()
+
+
 @pytest.mark.parametrize("n,most", [(60000, 100), (200000, 300), (200000, 8200)])
 def test_many_pages(n, most):
     """More pages than a workgroup has in registers, more picked than it lists; parts joined."""
