@@ -615,15 +615,17 @@ __device__ __forceinline__ void finish_run(const TreeArgs& a, const TreeRun& r, 
 
 // The parts of the rows that are shared, joined in their order: the same grid as the runs', and as many
 // workgroups as a row has parts take a share of its columns each.  (A join by the last of a row's
-// workgroups would read up to 4 MiB alone: 32 parts of 256 columns took 100 us.)
-constexpr int kJoinWaves = 8;
-
-template <int TT>
-__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) {
-  constexpr int W = kJoinWaves, NT = 64 * W;
+// workgroups would read up to 4 MiB alone: 32 parts of 256 columns took 100 us.)  Latency bounds it: the
+// plan, then the parts' maxima, then their sums, of which up to eight threads take a share (64 drafts of
+// 32768 tokens: 5.0 us, 7.1 with one thread for all parts).  Rows of one group have little to join: two
+// waves (384 rows in three parts: 9.8 us, 12 with eight waves).
+template <int TT, int W>
+__global__ __launch_bounds__(64 * W) void tree_join_kernel(TreeArgs a) {
+  constexpr int NT = 64 * W;
   constexpr int kPairs = kMostCols + kSmallGroups;  // columns / parts of them, for each part
   __shared__ int scan[2][W], found[4];
   __shared__ float weight[kPairs], sum[kPairs], top[kMostCols], total[kMostCols];
+  __shared__ v4f shares[NT];
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, block = (int)blockIdx.x;
   const int unit = (block >> 3) / a.blocks * 8 + (block & 7), cb = (block >> 3) % a.blocks;
@@ -643,7 +645,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) 
     for (int u = 0; u < U; ++u)
       v[u] = slot(min(q0 + u, parts - 1), min(y / (kD / 4), count - 1), 16 + 16 * (y % (kD / 4)));
   };
-  if (count > 0) fetch(tid, 0);
+  // Four channels a thread; where that leaves threads without any, up to eight share the parts.
+  const int items = count * (kD / 4);
+  const int split = count == 0 || 2 * items > NT ? 1 : 4 * items > NT ? 2 : 8 * items > NT ? 4 : 8;
+  const int per = (parts + split - 1) / split, mine = split > 1 ? tid / items : 0;
+  const int y0 = tid - mine * items, q_first = mine * per, q_last = min(q_first + per, parts);
+  if (count > 0 && mine < split) fetch(y0, q_first);
   for (int y = tid; y < count * parts; y += NT) {
     const v4f ml = slot(y % parts, y / parts, 0);
     weight[y] = ml[0];
@@ -671,20 +678,32 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a) 
     }
   }
   __syncthreads();
-  for (int y = tid; y < count * (kD / 4); y += NT) {
-    const int col = y / (kD / 4), c4 = y % (kD / 4);
+  auto joined = [&](int y) {
     v4f o = {0.f, 0.f, 0.f, 0.f};
-    for (int q0 = 0; q0 < parts; q0 += U) {
-      if (q0 > 0 || y != tid) fetch(y, q0);
+    for (int q0 = q_first; q0 < q_last; q0 += U) {
+      if (q0 > q_first || y != y0) fetch(y, q0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float w = q0 + u < parts ? weight[col * parts + q0 + u] : 0.f;
+        const float w = q0 + u < q_last ? weight[y / (kD / 4) * parts + q0 + u] : 0.f;
         if (w != 0.f) o += w * v[u];
       }
     }
-    const int column = cb * a.block_cols + first + col;
-    finish_column(a, r, column / p.G, column, c4, top[col], total[col], o);
+    return o;
+  };
+  auto finish = [&](int y, v4f o) {
+    const int col = y / (kD / 4), column = cb * a.block_cols + first + col;
+    finish_column(a, r, column / p.G, column, y % (kD / 4), top[col], total[col], o);
+  };
+  if (split == 1) {
+    for (int y = tid; y < items; y += NT) finish(y, joined(y));
+    return;
   }
+  if (mine < split) shares[tid] = joined(y0);
+  __syncthreads();
+  if (mine > 0) return;
+  v4f o = shares[tid];
+  for (int x = 1; x < split; ++x) o += shares[x * items + tid];
+  finish(tid, o);
 }
 
 // Up to 16 columns: every wave has tiles of its own; keys and values one tile ahead, pages two.  Few rows:
@@ -1031,8 +1050,11 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
   // (a table that holds no more than a shortest run's tokens has no shared rows)
   const int tt = full ? Full32<false>::kTokens : Half16<__bf16, false>::kTokens;
   if (e != AATC_OK || (a.p.len_max + a.drafts) / tt < kRoundsMin * a.quantum) return e;
-  return full ? launch(tree_join_kernel<Full32<false>::kTokens>, kJoinWaves)
-              : launch(tree_join_kernel<Half16<__bf16, false>::kTokens>, kJoinWaves);
+  if (small_groups(b, rows))
+    return full ? launch(tree_join_kernel<Full32<false>::kTokens, 2>, 2)
+                : launch(tree_join_kernel<Half16<__bf16, false>::kTokens, 2>, 2);
+  return full ? launch(tree_join_kernel<Full32<false>::kTokens, 8>, 8)
+              : launch(tree_join_kernel<Half16<__bf16, false>::kTokens, 8>, 8);
 }
 
 namespace {
