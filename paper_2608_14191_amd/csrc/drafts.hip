@@ -34,8 +34,9 @@ constexpr int kFewRows = 128, kSmallGroups = 1024;
 constexpr int kGroup = 16;                        // columns of a group
 constexpr int kMostCols = 128;                    // of a workgroup
 // Runs are a multiple of so many tiles, twice that at least: what a workgroup computes in about the time
-// that the join takes.
-constexpr int quantum_of(int cols) { return cols <= 64 ? 8 : 4; }
+// that the join takes.  `slow`: the wide kernel with four waves (648 tokens, 42 columns, float32 queries
+// over bf16: 19 us, 28 with 8; 924 float32 tokens, 20 columns: 19 and 29).
+constexpr int quantum_of(int cols, bool slow) { return slow ? 2 : cols <= 64 ? 8 : 4; }
 // The maximum that weights refer to is renewed when a score passes it by this much (exponents of 2):
 // sums and outputs are rescaled rarely.  Weights of 2^(slack + below) have to fit their type, and in
 // f16 small ones stay off the denormals.
@@ -1007,7 +1008,7 @@ aatc_status launch_tree(TreeArgs a, aatc_dtype c_dtype, void* workspace, void* s
   a.blocks = b.blocks;
   a.block_cols = b.cols();
   a.units = units_of(b, rows);
-  a.quantum = quantum_of(b.cols());
+  a.quantum = quantum_of(b.cols(), b.cols() > kGroup && (full || !same));
   a.p.parts = static_cast<Partial*>(workspace);
   const int64_t most = rows <= a.units ? a.units : (int64_t)rows + a.units;
   const int64_t grid = (most + 7) / 8 * 8 * b.blocks;
