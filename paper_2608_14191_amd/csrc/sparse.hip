@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
   constexpr int W = kSparseWaves, NT = 64 * W, TT = M::kTokens, NM = M::kMine;
   __shared__ JoinSpace<W, kSparseGroups> sh;
   __shared__ int list_entry[kListed], list_page[kListed];
-  __shared__ int hist[2][kBins], sums[3][W], found[3];
+  __shared__ int hist[2][kBins], sums[5][W], found[3];
   __shared__ unsigned arrived;
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -541,15 +541,15 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
     eq += ties && k == limit;
   });
   int gt_before = wave_scan_sum(gt), eq_before = wave_scan_sum(eq);
-  if (lane == 63) {
-    sums[1][wave] = gt_before;
-    sums[2][wave] = eq_before;
+  if (lane == 63) {                                // (rows of their own: other waves may still read the others)
+    sums[3][wave] = gt_before;
+    sums[4][wave] = eq_before;
   }
   __syncthreads();
   int gt_all = 0, eq_all = 0;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    const int x = sums[1][w], y = sums[2][w];
+    const int x = sums[3][w], y = sums[4][w];
     gt_before += w < wave ? x : 0;
     eq_before += w < wave ? y : 0;
     gt_all += x;
