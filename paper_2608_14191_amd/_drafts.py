@@ -53,13 +53,24 @@ def _trees(func: str, seq_len, n_draft, parent, batch: int, max_draft: int):
         _list(func, "parent", parent, batch * max_draft)
 
 
-def _draft_stride(func: str, q, batch: int, max_draft: int) -> int:
-    """Elements between drafts of a view [batch * max_draft][heads][128] or [batch][max_draft][...]."""
-    if q.dim() < 4 or max_draft == 1:
-        if q.shape[0] < batch * max_draft:
-            _refuse(func, f"q has {q.shape[0]} tokens of {batch * max_draft}")
+def _draft_stride(func: str, q, batch: int, max_draft: int, heads: int) -> int:
+    """Elements between the drafts of a tensor that lies packed, or whose first dimension is tokens,
+    [tokens][heads][128], or its first two are sequences and drafts, [batch][max_draft][...]; with
+    more heads than are read, each draft's first ones."""
+    n, width, packed = batch * max_draft, heads * HEAD_DIM, q.is_contiguous()
+    if n <= 1 or (packed and q.numel() == n * width):
+        return width
+    while q.dim() > 1 and q.shape[0] == 1:
+        q = q[0]
+    shape, dim = q.shape, q.dim()
+    if packed and (dim == 1 or q.stride(0) <= width):          # (tokens, or parts of them)
+        return width
+    two = dim > 3 or (packed and dim == 3 and not (shape[2] == HEAD_DIM and shape[0] >= n))
+    if not two or max_draft == 1:
+        if shape[0] < n:
+            _refuse(func, f"q has {shape[0]} tokens of {n}")
         return q.stride(0)
-    if q.shape[0] < batch or q.shape[1] != max_draft or \
+    if shape[0] < batch or shape[1] != max_draft or \
             (batch > 1 and q.stride(0) != max_draft * q.stride(1)):
         _refuse(func, f"q's {batch} x {max_draft} drafts do not lie at equal steps")
     return q.stride(1)
@@ -71,7 +82,8 @@ def aatc_paged_tree_attention(cache: PagedCache, table, seq_len, batch: int, max
                               sink: int = 0, softcap: float = 0.0, slopes=None, lse=None,
                               stream=None):
     """Attention of max_draft drafted tokens per sequence (q: batch * max_draft tokens of
-    [n_q_heads][128], q_tok_stride elements apart, by default as the tensor's strides have them)
+    [n_q_heads][128], q_tok_stride elements apart, by default as the tensor has them:
+    [tokens][n_q_heads][128], or [batch][max_draft][n_q_heads][128])
     over the pages; parent int32 [batch][max_draft] or None (a chain); out
     [batch][max_draft][n_q_heads][128] and lse [batch][max_draft][n_q_heads] in float32."""
     f = "aatc_paged_tree_attention"
@@ -84,9 +96,7 @@ def aatc_paged_tree_attention(cache: PagedCache, table, seq_len, batch: int, max
         _floats(f, "lse", lse, n * n_q_heads)
     if slopes is not None:
         _floats(f, "slopes", slopes, n_q_heads)
-    stride = n_q_heads * HEAD_DIM if q_tok_stride is None else q_tok_stride
-    if q_tok_stride is None and n > 1 and not q.is_contiguous():
-        stride = _draft_stride(f, q, batch, max_draft)
+    stride = _draft_stride(f, q, batch, max_draft, n_q_heads) if q_tok_stride is None else q_tok_stride
     _tokens(f, "q", q, n, stride, n_q_heads)
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), _ptr(n_draft), _ptr(parent), batch,
