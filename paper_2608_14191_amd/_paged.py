@@ -158,6 +158,21 @@ def _tokens(func: str, name: str, t, n_tok: int, stride: int, heads: int):
         _refuse(func, f"{name} holds {have} elements from its first on, {need} are used")
 
 
+def _row_stride(func: str, q, rows: int, heads: int) -> int:
+    """Elements between the rows of a tensor that lies packed, or whose first dimension is rows; with
+    more heads than are read, each row's first ones."""
+    width, packed = heads * HEAD_DIM, q.is_contiguous()
+    if rows <= 1 or (packed and q.numel() == rows * width):
+        return width
+    while packed and q.dim() > 1 and q.shape[0] == 1:
+        q = q[0]
+    if packed and (q.dim() == 1 or q.stride(0) <= width):      # (rows, or parts of them)
+        return width
+    if q.shape[0] < rows:
+        _refuse(func, f"q has {q.shape[0]} rows of {rows}")
+    return q.stride(0)
+
+
 def _table(func: str, table, device: int):
     """(aatc_page_table as an argument, rows) of a PageTable or an int32 tensor."""
     handle = isinstance(table, PageTable)
@@ -309,11 +324,7 @@ def aatc_paged_decode_attention(cache: PagedCache, table, seq_len, batch: int, n
         _floats(f, "lse", lse, batch * n_q_heads)
     if slopes is not None:
         _floats(f, "slopes", slopes, n_q_heads)
-    stride = n_q_heads * HEAD_DIM if q_stride is None else q_stride
-    if q_stride is None and batch > 1 and not q.is_contiguous():
-        if q.shape[0] < batch:
-            _refuse(f, f"q has {q.shape[0]} rows of {batch}")
-        stride = q.stride(0)
+    stride = _row_stride(f, q, batch, n_q_heads) if q_stride is None else q_stride
     _tokens(f, "q", q, batch, stride, n_q_heads)
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), batch, n_q_heads, q.data_ptr(),
@@ -341,7 +352,8 @@ def aatc_decode_attention_paged(dev_params_k, dev_params_v, batch: int, n_q_head
     _list(f, "seq_len", seq_len, batch)
     _list(f, "page_len", page_len, batch)
     _floats(f, "out", out, batch * n_q_heads * HEAD_DIM)
-    if not q.is_contiguous() or q.numel() < batch * n_q_heads * HEAD_DIM:
+    if not q.is_contiguous() or q.numel() < batch * n_q_heads * HEAD_DIM or \
+            _row_stride(f, q, batch, n_q_heads) != n_q_heads * HEAD_DIM:
         _refuse(f, "q must be a contiguous tensor [batch][n_q_heads][128]")
     params, tokens = _lib.aatc_params_bytes(n_kv_heads), batch * n_kv_heads * cap
     _buffer(f, "dev_params_k", dev_params_k, params)

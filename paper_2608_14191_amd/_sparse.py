@@ -10,8 +10,8 @@ import ctypes
 
 from . import _lib, _paged
 from ._lib import HEAD_DIM, AatcError
-from ._paged import (PagedCache, _dtype, _floats, _list, _on_device, _ptr, _refuse, _space, _table,
-                     _tokens)
+from ._paged import (PagedCache, _dtype, _floats, _list, _on_device, _ptr, _refuse, _row_stride, _space,
+                     _table, _tokens)
 
 _vp, _i32, _i64, _sz, _f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                               ctypes.c_float)
@@ -86,11 +86,7 @@ def aatc_paged_sparse_attention(cache: PagedCache, table, seq_len, codes, scales
     _floats(f, "out", out, batch * n_q_heads * HEAD_DIM)
     if lse is not None:
         _floats(f, "lse", lse, batch * n_q_heads)
-    stride = n_q_heads * HEAD_DIM if q_stride is None else q_stride
-    if q_stride is None and batch > 1 and not q.is_contiguous():
-        if q.shape[0] < batch:
-            _refuse(f, f"q has {q.shape[0]} rows of {batch}")
-        stride = q.stride(0)
+    stride = _row_stride(f, q, batch, n_q_heads) if q_stride is None else q_stride
     _tokens(f, "q", q, batch, stride, n_q_heads)
     t, _ = _table(f, table, device)
     status = entry_point(f)(cache.address, t, seq_len.data_ptr(), codes.data_ptr(), scales.data_ptr(),
