@@ -37,13 +37,15 @@ constexpr int kMostCols = 128;                    // of a workgroup
 // that the join takes.  `slow`: the wide kernel with four waves (648 tokens, 42 columns, float32 queries
 // over bf16: 19 us, 28 with 8; 924 float32 tokens, 20 columns: 19 and 29).
 constexpr int quantum_of(int cols, bool slow) { return slow ? 2 : cols <= 64 ? 8 : 4; }
-// The maximum that weights refer to is renewed when a score passes it by this much (exponents of 2):
-// sums and outputs are rescaled rarely.  Weights of 2^(slack + below) have to fit their type, and in
-// f16 small ones stay off the denormals.
+// Weights are powers of 2 relative to a reference that is renewed when a weight would pass 2^kMost, and
+// then so that the highest one is 2^kFirst: sums and outputs are rescaled rarely (when a score rises by
+// 8, in f16 6).  bf16 and float32: weights of at most 1, so that sums stay as far from float32's range
+// as those of one token's attention.  f16: its values leave room, and small weights stay off the
+// denormals.
 template <class M>
-constexpr float kSlack = std::is_same_v<typename M::Elem, _Float16> ? 6.f : 8.f;
+constexpr float kMost = std::is_same_v<typename M::Elem, _Float16> ? 15.f : 0.f;
 template <class M>
-constexpr float kBelow = std::is_same_v<typename M::Elem, _Float16> ? 9.f : 0.f;
+constexpr float kFirst = std::is_same_v<typename M::Elem, _Float16> ? 9.f : -8.f;
 
 // The window that the shallowest and the deepest of m drafts have together.
 __host__ __device__ inline int window_of(int window, int m) {
@@ -440,13 +442,13 @@ struct TreeWave {
       top[c] = z[c][0];
 #pragma unroll
       for (int e = 1; e < NM; ++e) top[c] = fmaxf(top[c], z[c][e]);
-      higher |= top[c] * unit - kBelow<M> > m_run[c] + kSlack<M>;
+      higher |= top[c] * unit > m_run[c] + kMost<M>;
     }
     if (__builtin_amdgcn_ballot_w64(higher)) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const float most = over_groups_max(top[c]) * unit - kBelow<M>;
-        const float next = most > m_run[c] + kSlack<M> ? most : m_run[c];
+        const float most = over_groups_max(top[c]) * unit;
+        const float next = most > m_run[c] + kMost<M> ? most - kFirst<M> : m_run[c];
         const float ref = next == -INFINITY ? 0.f : next;
         const float sa = __builtin_amdgcn_exp2f(m_run[c] - ref);    // (0 at the first tile)
         l_run[c] *= sa;
