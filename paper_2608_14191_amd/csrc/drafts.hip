@@ -47,6 +47,11 @@ constexpr float kMost = std::is_same_v<typename M::Elem, _Float16> ? 15.f : 0.f;
 template <class M>
 constexpr float kFirst = std::is_same_v<typename M::Elem, _Float16> ? 9.f : -8.f;
 
+// With references from here on (exponents of 2) scores are scaled and rounded before the reference is taken
+// off, as on every other path: a fused product keeps bits that the reference, itself rounded, has not.
+// They are half a last place of the score: 2^-17 of a weight here, but 2^128 of one from 2^32 on.
+constexpr float kLarge = 256.f;
+
 // The window that the shallowest and the deepest of m drafts have together.
 __host__ __device__ inline int window_of(int window, int m) {
   return window > 0 ? min(window, 1 << 30) + m - 1 : 0;
@@ -297,10 +302,12 @@ struct TreeWave {
   float m_run[C], l_run[C];
   unsigned seen = 0u;                              // bit c: any token attended by the lane's column
   bool odd = false;                                // values that are not finite in a masked tile
+  bool plain;                                      // scores are only scaled, references below kLarge
 
   __device__ TreeWave(const TreeArgs& a, const TreeRun& r, TreeInfo& space, int block, int first,
                       int columns)
-      : p(a.p), info(space), col0(first), len(r.len), end(r.len + r.m) {
+      : p(a.p), info(space), col0(first), len(r.len), end(r.len + r.m),
+        plain(a.p.cap == 0.f && !a.p.slopes && a.p.scale > 0.f) {
     lo = p.window > 0 ? max(0, end - window_of(p.window, r.m)) : 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -428,7 +435,7 @@ struct TreeWave {
     for (int c = 0; c < C; ++c) M::template scores<QT>(key, q[c], z[c]);
     next_keys();
     float unit = p.scale * kLog2e;                 // (scores that are only scaled are so on the way)
-    if (whole && p.cap == 0.f && !p.slopes && p.scale > 0.f) {
+    if (whole && plain) {
       seen = ~0u;
     } else {
       unit = 1.f;
@@ -445,16 +452,26 @@ struct TreeWave {
       higher |= top[c] * unit > m_run[c] + kMost<M>;
     }
     if (__builtin_amdgcn_ballot_w64(higher)) {
+      bool far = false;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const float most = over_groups_max(top[c]) * unit;
         const float next = most > m_run[c] + kMost<M> ? most - kFirst<M> : m_run[c];
         const float ref = next == -INFINITY ? 0.f : next;
+        far |= !(fabsf(ref) < kLarge);
         const float sa = __builtin_amdgcn_exp2f(m_run[c] - ref);    // (0 at the first tile)
         l_run[c] *= sa;
         m_run[c] = next;
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] *= sa;
+      }
+      if (__builtin_amdgcn_ballot_w64(far)) {
+        plain = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < NM; ++e) z[c][e] *= unit;
+        unit = 1.f;
       }
     }
 #pragma unroll
