@@ -457,6 +457,15 @@ struct Full32 {
   }
 };
 
+// What the weights of scores up to `top` (exponents of 2) are relative to: kLower below it, so that small
+// ones stay off f16's denormals; the score itself where the difference, rounded to the places of large
+// scores (from 2^25 on), would leave weights of 2^16, beyond f16.
+template <class M>
+__device__ inline float reference_of(float top) {
+  const float low = top - M::kLower;
+  return M::kLower > 0.f && top - low > 15.f ? top : low;
+}
+
 // tanh to a few ulps: for small |x| the first terms of its odd series (the next is 4e-8 of x at
 // 0.55), else from exp(-2 |x|).
 __device__ inline float tanh_of(float x) {

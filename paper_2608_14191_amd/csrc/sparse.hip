@@ -655,7 +655,7 @@ __global__ __launch_bounds__(64 * kSparseWaves, 2) void sparse_kernel(SparseArgs
     float m = z[0];
 #pragma unroll
     for (int e = 1; e < NM; ++e) m = fmaxf(m, z[e]);
-    m = fmaxf(m_run, over_groups_max(m) - M::kLower);
+    m = fmaxf(m_run, reference_of<M>(over_groups_max(m)));
     const float ref = m == -INFINITY ? 0.f : m;
     const float sa = __builtin_amdgcn_exp2f(m_run - ref);      // (0 at the first tile)
     float w[NM], sum = 0.f;
