@@ -72,7 +72,8 @@ aatc_status aatc_paged_tree_attention(const aatc_paged_cache* cache, const aatc_
  * sequences (aatc_pages_reserve sees to that).
  *
  * cache        of the first layer; layer l's pools are l * layer_stride elements behind its, in both.
- * n_layers     1 .. 65535.  layer_stride: elements, a multiple of 16 bytes (not read for one layer).
+ * n_layers     1 .. 65535, for up to 65535 KV heads.
+ * layer_stride elements, a multiple of 16 bytes (not read for one layer).
  * drafted      device [batch][max_draft] int32, the drafts' tokens.
  * chosen       device [batch][max_draft] int32.
  * path         device [batch][max_draft] int32: the accepted drafts, ascending, -1 behind them.
@@ -81,7 +82,8 @@ aatc_status aatc_paged_tree_attention(const aatc_paged_cache* cache, const aatc_
  * len_out      device [batch] int32: seq_len, clamped as below, + accepted.
  * No output overlaps an input or another output: AATC_E_INVALID.
  * seq_len, n_draft, parent, max_draft: as in aatc_paged_tree_attention (seq_len clamped likewise).
- * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; max_draft), AATC_E_DEVICE.
+ * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; max_draft; n_layers * n_kv_heads over 2^34 bytes
+ * of d elements: 2^26, or 2^25 in float32), AATC_E_DEVICE.
  */
 aatc_status aatc_paged_tree_accept(const aatc_paged_cache* cache, int32_t n_layers,
                                    int64_t layer_stride, const aatc_page_table* table,

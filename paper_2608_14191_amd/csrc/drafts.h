@@ -12,6 +12,7 @@ namespace aatc {
 constexpr int kMaxDrafts = AATC_MAX_DRAFTS;       // a lane, and a bit of 64, for each
 constexpr int kMaxColumns = 16384;                // queries of a (sequence, KV head)
 constexpr int64_t kMaxTreeGroups = (int64_t)1 << 22;
+constexpr int64_t kMaxMoved = (int64_t)1 << 31;   // 16-byte pieces of a token, of all layers: a thread each
 
 struct TreeArgs {
   PagedArgs p;                    // q_stride: from draft to draft

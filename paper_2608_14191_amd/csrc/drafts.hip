@@ -1156,9 +1156,8 @@ __global__ __launch_bounds__(256) void accept_kernel(AcceptArgs a) {
 
 aatc_status launch_tree_accept(const AcceptArgs& a, void* stream) {
   const int64_t pieces = (int64_t)a.layers * 2 * a.n_kv_heads * a.pieces;
-  const int64_t groups = (pieces + 255) / 256;
+  const int64_t groups = (pieces + 255) / 256;     // (2^23 at most)
   constexpr int kMost = 65535;                     // sequences of a launch
-  if (groups > (1 << 23)) return AATC_E_UNSUPPORTED;
   for (int b = 0; b < a.batch; b += kMost) {
     AcceptArgs s = a;
     const int64_t at = (int64_t)b * a.drafts;

@@ -93,6 +93,8 @@ extern "C" aatc_status aatc_paged_tree_accept(
     if (n_layers > 1 && (layer_stride < kD || layer_stride % (16 / size) ||
                          layer_stride >= ((int64_t)1 << 40)))
       return AATC_E_INVALID;
+    const int pieces = kD * size / 16;
+    if ((int64_t)n_layers * 2 * cache->n_kv_heads * pieces > kMaxMoved) return AATC_E_UNSUPPORTED;
     // (every workgroup of a sequence reads the inputs: no output overlaps one, or another)
     const int64_t each = (int64_t)batch * max_draft;
     const List in[] = {{drafted, each}, {chosen, each}, {seq_len, batch}, {n_draft, batch},
@@ -132,7 +134,7 @@ extern "C" aatc_status aatc_paged_tree_accept(
     a.max_pages = table->max_pages;
     a.page_shift = log2_of(cache->page_tokens);
     a.len_max = (int)row_tokens(*table, cache->page_tokens);
-    a.pieces = kD * size / 16;
+    a.pieces = pieces;
     return launch_tree_accept(a, stream);
   } catch (...) {
     return AATC_E_INVALID;
