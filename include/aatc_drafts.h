@@ -49,7 +49,8 @@ extern "C" {
  *           Calls that may overlap need one each.
  * Other arguments as in aatc_paged_decode_attention.
  * Errors: AATC_E_INVALID, AATC_E_UNSUPPORTED (d != 128; max_draft; more than 2^30 tiles of 16 tokens;
- * max_draft * n_q_heads / n_kv_heads over 16384), AATC_E_WORKSPACE, AATC_E_DEVICE.
+ * c = max_draft * n_q_heads / n_kv_heads over 16384; (batch * n_kv_heads + 1032) ceil(c / 128) over
+ * 2^22), AATC_E_WORKSPACE, AATC_E_DEVICE.
  */
 size_t aatc_paged_tree_workspace_bytes(int32_t batch, int32_t max_draft, int32_t n_q_heads,
                                        int32_t n_kv_heads);

@@ -64,7 +64,8 @@ aatc_status aatc_page_bounds(const aatc_paged_cache* cache, const aatc_page_tabl
  *            it reusable, for calls of other shapes that it is large enough for too.  Calls that may
  *            overlap need one each.
  * Other arguments and errors as in aatc_paged_decode_attention; AATC_E_UNSUPPORTED also for
- * batch * n_kv_heads * max_pages over 2^30, most over 2^20, and over 256 query heads a KV head.
+ * batch * n_kv_heads * max_pages over 2^30, batch * n_kv_heads times ceil(max_pages / 64) or times
+ * ceil(n_q_heads / n_kv_heads / 16) over 2^22, most over 2^20, and over 256 query heads a KV head.
  */
 size_t aatc_paged_sparse_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                          int64_t max_pages);
