@@ -34,8 +34,10 @@ constexpr int kFewRows = 128, kSmallGroups = 1024;
 constexpr int kGroup = 16;                        // columns of a group
 constexpr int kMostCols = 128;                    // of a workgroup
 // Runs are a multiple of so many tiles, twice that at least: what a workgroup computes in about the time
-// that the join takes.  `slow`: the wide kernel with four waves (648 tokens, 42 columns, float32 queries
-// over bf16: 19 us, 28 with 8; 924 float32 tokens, 20 columns: 19 and 29).
+// that the join takes.  `slow`: the wide kernel with four waves, one a SIMD.  (648 tokens, 42 columns,
+// float32 queries over bf16: 19 us, 28 with the others' 8; 924 float32 tokens, 20 columns: 19 and 28; 2 x
+// 600, 371 columns: 38 and 44; 16 x 400, 280 columns: 88 and 90.  It loses where short rows fill the chip
+// as they are: 11 x 290 float32 tokens, 371 columns: 65 and 60.)
 constexpr int quantum_of(int cols, bool slow) { return slow ? 2 : cols <= 64 ? 8 : 4; }
 // Weights are powers of 2 relative to a reference that is renewed when a weight would pass 2^kMost, and
 // then so that the highest one is 2^kFirst: sums and outputs are rescaled rarely (when a score rises by
@@ -728,8 +730,8 @@ __global__ __launch_bounds__(64 * W) void tree_join_kernel(TreeArgs a) {
 }
 
 // Up to 16 columns: every wave has tiles of its own; keys and values one tile ahead, pages two.  Few rows:
-// eight waves a workgroup, so that a row has few parts to join.  Many: four, whose runs are dealt more
-// evenly (384 rows of 129 float32 tiles: 157 us, eight 165).
+// eight waves a workgroup, so that a row has few parts to join.  Many: four, four times as many workgroups,
+// whose runs are dealt more evenly (384 rows of 129 float32 tiles: 145 us with the join, 172 with eight).
 template <class M, int QT, int W>
 __global__ __launch_bounds__(64 * W, 2) void tree_narrow_kernel(TreeArgs a) {
   constexpr int TT = M::kTokens, NM = M::kMine;
@@ -781,8 +783,9 @@ __global__ __launch_bounds__(64 * W, 2) void tree_narrow_kernel(TreeArgs a) {
                    std::integral_constant<int, 1>{});
 }
 
-// More columns.  A stage has kStage tiles: 16 KiB of keys and 16 KiB of values, loaded straight into
-// LDS, kRing - 1 stages ahead of the one that is computed.  Wave w has 16 C columns from
+// More columns: eight waves a workgroup, two a SIMD, or four where registers leave room for one.  A stage has
+// kStage tiles, each 8 KiB of keys and 8 KiB of values, loaded straight into LDS, kRing - 1 stages ahead of
+// the one that is computed.  Wave w has 16 C columns from
 // (w / TW) 16 C on and every TW-th tile.
 constexpr int kRingTiles = 8;
 constexpr int kStreamed = 2;                       // cache policy nt
@@ -983,10 +986,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void tree_wide_kernel(TreeArgs a) {
                     std::integral_constant<int, C>{});
 }
 
-// A (sequence, KV head)'s columns in blocks of nearly as many groups each; a block's groups are dealt
-// to `cw` sets of waves, c groups each.  (Blocks of 256 columns, which read keys and values half as
-// often but have twice the parts to join, took as long for 64 drafts of 32768 tokens and longer for
-// fewer tokens: 28.3 us at 1000 tokens, 33.7.)
+// A (sequence, KV head)'s columns in blocks of 32, 64 or 128, the smallest that hold an even share; the
+// first are full, the last has the rest.  A block's groups are dealt to `cw` sets of waves, c groups each.
+// (Blocks of 256 columns, which read keys and values half as often but have twice the parts to join, took
+// as long for 64 drafts of 32768 tokens and longer for fewer tokens: 28.3 us at 1000 tokens, 33.7.)
 struct Blocks {
   int blocks, c, cw;
   int cols() const { return c * cw * kGroup; }
