@@ -8,6 +8,7 @@ raises ImportError: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import re
 
@@ -66,7 +67,20 @@ class Calibration(ctypes.Structure):
 LIB_PATH = os.environ.get("AATC_LIBRARY", LIB)   # optional override of the built library
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; call __graft_entry__.build() first")
-_L = ctypes.CDLL(LIB_PATH)
+
+
+def _load(path: str):
+    """The library, over the HIP runtime that torch brings: two of them in a process would not know each
+    other's memory and streams, and the one that is loaded first serves both."""
+    torch = importlib.util.find_spec("torch")          # (found, not imported)
+    if torch is not None and torch.origin:
+        runtime = os.path.join(os.path.dirname(torch.origin), "lib", "libamdhip64.so")
+        if os.path.exists(runtime):
+            ctypes.CDLL(runtime)
+    return ctypes.CDLL(path)
+
+
+_L = _load(LIB_PATH)
 
 _vp, _i32, _i64, _sz, _f32, _f64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                     ctypes.c_size_t, ctypes.c_float, ctypes.c_double)
